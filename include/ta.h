@@ -338,6 +338,48 @@ int ta_forward_static(const void *q, const void *k, const void *v, void *out,
                       const int *dims, int ndims, int causal, int dtype, ta_stream_t stream);
 
 /*
+ * Rotary positions with several axes (Section 3.2: a token's position is the vector of its coordinates): pairs of
+ * features of every q and k row are turned once, before attention, by angles that come from one of several
+ * coordinates of the token -- the coordinates of the n_1 x ... x n_m tensor, or time / height / width positions
+ * given per token.  (ta_forward_ex's rope_base is the other reading: every hop rotates all features by the hop's own
+ * coordinate.)  A head of D features consists of `parts` parts of D / parts features, all rotated alike (1; 2 for
+ * ta_diff_forward, whose two maps each use one half of the features).  In a part, pair c belongs to axis a(c) --
+ * sections[0] pairs to axis 0, the next sections[1] to axis 1, ... -- and is turned by
+ *     angle = position[a(c)] * base^(-c / P)                     P = sum(sections)
+ *     angle = position[a(c)] * base^(-(c - start_a) / sections[a])   with per_axis_ladder
+ *     y1 = x1 cos - x2 sin,  y2 = x2 cos + x1 sin
+ * where (x1, x2) are features (c, c + P) of the part, or (2c, 2c+1) with `interleaved`.  Features from 2 P on are
+ * copied.  Angles are exact modulo a turn for every 32-bit position; arithmetic is fp32, rounded once.  With
+ * `inverse` the angles change sign: the gradient with respect to q, k from the gradient of the rotated ones (and the
+ * inverse of the rotation).
+ */
+typedef struct ta_rotary_params {
+    size_t struct_bytes;        /* sizeof(ta_rotary_params)                                         */
+    const void *q, *k;          /* device: [B,H,N,D], [B,H_kv,N,D]; k NULL exactly when H_kv == 0    */
+    void *q_out, *k_out;        /* device; each may be its own input (same address and strides),     */
+                                /* but share no memory with another tensor of the call               */
+    int B, H, H_kv, N, D;       /* D <= TA_MAX_HEAD_DIM, D % parts == 0                              */
+    int dtype;                  /* TA_DTYPE_*                                                        */
+    int parts;
+    const int *sections;        /* host, naxes ints >= 0; 1 <= sum, 2 * sum <= D / parts             */
+    int naxes;                  /* 1 .. TA_MAX_DIMS                                                  */
+    const int *positions;       /* DEVICE, [naxes][B][N], or NULL: then dims is given                */
+    long long pos_axis_stride;  /* elements between axes                                             */
+    long long pos_batch_stride; /* elements between batch entries (0: the same for all)              */
+    const int *dims;            /* host, naxes ints, or NULL: token n stands at the row-major        */
+    long long token_offset;     /* coordinates of index token_offset + n in this tensor              */
+    double base;                /* > 0 (Llama: 10000)                                                */
+    int interleaved, per_axis_ladder, inverse;
+    long long q_strides[3], k_strides[3];         /* elements between batch entries, heads, tokens;  */
+    long long q_out_strides[3], k_out_strides[3]; /* all 0: contiguous.  D is always innermost       */
+    ta_stream_t stream;
+} ta_rotary_params;
+
+/* Alignment: every address and stride a multiple of the element; 16-byte aligned rows (and, without `interleaved`,
+ * sum(sections) * element size a multiple of 16) run with 16-byte accesses, others with narrower ones. */
+int ta_rotary(const ta_rotary_params *p);
+
+/*
  * Text description of the launch plan the library would use for a problem (one line per hop:
  * kernel path -- tc, tc-fused, tc-long or simt --, segment length, stride, tile packing,
  * source / destination buffer).  Pure

@@ -26,7 +26,7 @@ TA_WS_FORWARD, TA_WS_FORWARD_SAVE, TA_WS_BACKWARD, TA_WS_BACKWARD_F32_GRADS = 0,
 EXPORTS = ("ta_forward", "ta_forward_f32", "ta_forward_ex", "ta_backward", "ta_workspace_bytes",
            "ta_forward_host", "ta_plan_describe", "ta_device_status", "ta_launch_count",
            "ta_release", "ta_status_string", "ta_version", "ta_forward_static", "ta_backward_ex",
-           "ta_last_cuda_error", "ta_selftest_wait_timeout")
+           "ta_last_cuda_error", "ta_selftest_wait_timeout", "ta_rotary")
 TA_STATIC_SCRATCH_BYTES = 16 << 20
 
 
@@ -77,6 +77,24 @@ class ta_bwd_params(ctypes.Structure):
                 ("stream", ctypes.c_void_p)]
 
 
+class ta_rotary_params(ctypes.Structure):
+    _fields_ = [("struct_bytes", ctypes.c_size_t),
+                ("q", ctypes.c_void_p), ("k", ctypes.c_void_p),
+                ("q_out", ctypes.c_void_p), ("k_out", ctypes.c_void_p),
+                ("B", ctypes.c_int), ("H", ctypes.c_int), ("H_kv", ctypes.c_int),
+                ("N", ctypes.c_int), ("D", ctypes.c_int),
+                ("dtype", ctypes.c_int), ("parts", ctypes.c_int),
+                ("sections", ctypes.POINTER(ctypes.c_int)), ("naxes", ctypes.c_int),
+                ("positions", ctypes.c_void_p),
+                ("pos_axis_stride", ctypes.c_longlong), ("pos_batch_stride", ctypes.c_longlong),
+                ("dims", ctypes.POINTER(ctypes.c_int)), ("token_offset", ctypes.c_longlong),
+                ("base", ctypes.c_double),
+                ("interleaved", ctypes.c_int), ("per_axis_ladder", ctypes.c_int), ("inverse", ctypes.c_int),
+                ("q_strides", ctypes.c_longlong * 3), ("k_strides", ctypes.c_longlong * 3),
+                ("q_out_strides", ctypes.c_longlong * 3), ("k_out_strides", ctypes.c_longlong * 3),
+                ("stream", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -114,6 +132,7 @@ def load():
     lib.ta_last_cuda_error.argtypes = []
     lib.ta_last_cuda_error.restype = ctypes.c_int
     lib.ta_version.argtypes = []
+    lib.ta_rotary.argtypes = [ctypes.POINTER(ta_rotary_params)]
     for name in EXPORTS:
         getattr(lib, name)          # every symbol of include/ta.h must be exported
     _lib = lib
@@ -298,6 +317,40 @@ def ta_backward_ex(dout, q, k, v, dq, dk, dv, B, H, H_kv, N, D, dims, causal,
     p.workspace, p.workspace_bytes = _ptr(workspace), workspace_bytes
     p.stream = _stream(stream)
     return _done(load().ta_backward_ex(ctypes.byref(p)), "ta_backward_ex", check)
+
+
+def _strides(strides, where):
+    """(batch, head, token) strides in elements as a C array; None: contiguous."""
+    s = (0, 0, 0) if strides is None else [int(x) for x in strides]
+    if len(s) != 3:
+        raise ValueError(f"{where} needs three strides: batch, head, token")
+    return (ctypes.c_longlong * 3)(*s)
+
+
+def ta_rotary(q, k, q_out, k_out, B, H, H_kv, N, D, sections, positions=None, pos_axis_stride=None,
+              pos_batch_stride=None, dims=None, token_offset=0, base=10000.0, parts=1, interleaved=False,
+              per_axis_ladder=False, inverse=False, dtype=TA_DTYPE_BF16, q_strides=None, k_strides=None,
+              q_out_strides=None, k_out_strides=None, stream=None, check=True) -> int:
+    """Rotary positions with several axes; positions: device int32 [naxes, B, N], or dims (coordinates of the token)."""
+    p = ta_rotary_params()
+    p.struct_bytes = ctypes.sizeof(ta_rotary_params)
+    p.q, p.k, p.q_out, p.k_out = _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out)
+    p.B, p.H, p.H_kv, p.N, p.D = B, H, H_kv, N, D
+    p.dtype, p.parts = dtype, parts
+    p.sections, p.naxes = _dims(sections)
+    p.positions = _ptr(positions)
+    p.pos_axis_stride = B * N if pos_axis_stride is None else pos_axis_stride
+    p.pos_batch_stride = N if pos_batch_stride is None else pos_batch_stride
+    if dims is not None:
+        if len(dims) != len(sections):
+            raise ValueError("dims and sections need one entry per axis")
+        p.dims = _dims(dims)[0]
+    p.token_offset, p.base = token_offset, base
+    p.interleaved, p.per_axis_ladder, p.inverse = int(bool(interleaved)), int(bool(per_axis_ladder)), int(bool(inverse))
+    p.q_strides, p.k_strides = _strides(q_strides, "q"), _strides(k_strides, "k")
+    p.q_out_strides, p.k_out_strides = _strides(q_out_strides, "q_out"), _strides(k_out_strides, "k_out")
+    p.stream = _stream(stream)
+    return _done(load().ta_rotary(ctypes.byref(p)), "ta_rotary", check)
 
 
 def ta_workspace_bytes(B, H, H_kv, N, D, dims, dtype=TA_DTYPE_BF16, mode=TA_WS_FORWARD) -> int:

@@ -1,4 +1,5 @@
-"""torch.autograd binding of the C-ABI library: ``tensorized_attention(q, k, v, dims, ...)``.
+"""torch.autograd binding of the C-ABI library: ``tensorized_attention(q, k, v, dims, ...)`` and
+``multi_axis_rotary(q, k, sections, ...)``.
 
 Marshalling only.  The forward is ``ta_forward_ex`` (with ``TA_FLAG_SAVE_HOPS`` when a gradient is
 needed, so the hop inputs X_1..X_{m-1} are kept instead of recomputed), the backward is
@@ -99,3 +100,103 @@ def tensorized_attention(q, k, v, dims, causal=True, softmax_scale=None, rope_ba
         _FN = _function()
     return _FN.apply(q, k, v, tuple(int(x) for x in dims), bool(causal), softmax_scale, rope_base, window,
                      hop_masks, seq_lens)
+
+
+def _strides3(t):
+    return t.stride(0), t.stride(1), t.stride(2)
+
+
+def _row_strided(t):
+    """The tensor itself when the library can address it (innermost features adjacent), else a contiguous copy."""
+    return t if t.stride(3) == 1 or t.shape[3] == 1 else t.contiguous()
+
+
+def _check_rotary(q, k, sections, positions, dims):
+    import torch
+    if not q.is_cuda or (k is not None and k.device != q.device):
+        raise ValueError("multi_axis_rotary needs CUDA tensors on one device (there is no CPU path)")
+    if q.dim() != 4 or (k is not None and k.dim() != 4):
+        raise ValueError("expected q [B,H,N,D] and k [B,H_kv,N,D]")
+    B, H, N, D = q.shape
+    if k is not None and (k.shape[0] != B or k.shape[2] != N or k.shape[3] != D):
+        raise ValueError("q and k disagree in batch, length or head dim")
+    if q.dtype not in (torch.bfloat16, torch.float32) or (k is not None and k.dtype != q.dtype):
+        raise ValueError("q, k must both be bfloat16 or both float32")
+    if (positions is None) == (dims is None):
+        raise ValueError("give either positions or dims")
+    if positions is not None:
+        if positions.dtype != torch.int32 or positions.device != q.device:
+            raise ValueError("positions must be int32 on the device of q")
+        if tuple(positions.shape) not in ((len(sections), B, N), (len(sections), N)):
+            raise ValueError("positions must have shape [axes, B, N] or [axes, N]")
+
+
+def _rotary_call(q, k, sections, positions, dims, token_offset, base, parts, interleaved, per_axis_ladder, inverse):
+    import torch
+    B, H, N, D = q.shape
+    q = _row_strided(q)
+    q_out = torch.empty((B, H, N, D), dtype=q.dtype, device=q.device)
+    k_out, H_kv = None, 0
+    if k is not None:
+        k = _row_strided(k)
+        H_kv = k.shape[1]
+        k_out = torch.empty((B, H_kv, N, D), dtype=q.dtype, device=q.device)
+    axis = batch = 0
+    if positions is not None:
+        if positions.stride(-1) != 1 and N > 1:
+            positions = positions.contiguous()
+        axis = positions.stride(0)
+        batch = positions.stride(1) if positions.dim() == 3 else 0
+    if q_out.numel() == 0:
+        return q_out, torch.empty_like(k) if k is not None else None
+    with torch.cuda.device(q.device):
+        ta.ta_rotary(q, k, q_out, k_out, B, H, H_kv, N, D, sections, positions=positions, pos_axis_stride=axis,
+                     pos_batch_stride=batch, dims=dims, token_offset=token_offset, base=base, parts=parts,
+                     interleaved=interleaved, per_axis_ladder=per_axis_ladder, inverse=inverse,
+                     dtype=ta.TA_DTYPE_BF16 if q.dtype == torch.bfloat16 else ta.TA_DTYPE_F32,
+                     q_strides=_strides3(q), k_strides=None if k is None else _strides3(k))
+    return q_out, k_out
+
+
+_ROTARY = None
+
+
+def _rotary_function():
+    import torch
+
+    class _MultiAxisRotary(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, positions, args):
+            ctx.save_for_backward(positions)
+            ctx.args = args
+            return _rotary_call(q, k, args[0], positions, *args[1:], False)
+
+        @staticmethod
+        def backward(ctx, dq, dk):
+            (positions,) = ctx.saved_tensors
+            dq, dk = _rotary_call(dq, dk, ctx.args[0], positions, *ctx.args[1:], True)
+            return dq, dk, None, None
+
+    return _MultiAxisRotary
+
+
+def multi_axis_rotary(q, k, sections, positions=None, dims=None, token_offset=0, base=10000.0, parts=1,
+                      interleaved=False, per_axis_ladder=False):
+    """Rotary positions with several axes: returns the rotated (q, k), differentiable with respect to both.
+
+    q: [B, H, N, D]; k: [B, H_kv, N, D] or None; bfloat16 or float32, innermost features adjacent.  sections: pairs of
+    features per axis.  positions: int32 [axes, B, N] (or [axes, N]); or dims: token n stands at the coordinates of
+    index token_offset + n in this tensor.  parts: sub-heads per head, rotated alike (2 for differential_attention).
+    interleaved: pairs (2c, 2c+1) instead of (c, c + P).  per_axis_ladder: a ladder of frequencies of its own per axis
+    instead of one over all pairs.  The results are contiguous.
+    """
+    global _ROTARY
+    sections = [int(x) for x in sections]
+    dims = None if dims is None else [int(x) for x in dims]
+    _check_rotary(q, k, sections, positions, dims)
+    args = (sections, dims, int(token_offset), float(base), int(parts), bool(interleaved), bool(per_axis_ladder))
+    if not q.requires_grad and (k is None or not k.requires_grad):
+        return _rotary_call(q, k, sections, positions, *args[1:], False)
+    if _ROTARY is None:
+        _ROTARY = _rotary_function()
+    return _ROTARY.apply(q, k, positions, args)

@@ -432,7 +432,7 @@ struct HostPipe {
 static HostPipe g_host_pipe;
 static std::mutex g_host_mutex;   // ta_forward_host calls, one at a time; taken before g_arena_mutex
 
-static int check_arch() {
+int check_arch() {
     static std::atomic<int> cached[64];   // 0 = unknown, 1 = compute capability 10.x, 2 = another
     int dev = 0, major = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) {

@@ -249,6 +249,16 @@ inline int launch_kernel(void (*kern)(KArgs...), unsigned grid, unsigned block, 
     return TA_OK;
 }
 
+// TA_OK when the calling thread's current device is compute capability 10.x, else TA_ERR_ARCH / TA_ERR_CUDA.
+int check_arch();
+// Strided [B][heads][N][D] tensors (strides in elements: batch, head, token; D innermost).  Strides of a contiguous
+// one where the caller gave only zeros.
+void take_strides(const long long *given, int heads, int N, int D, long long *s);
+// bytes [lo, hi) such a tensor spans
+void strided_extent(const void *p, const long long *s, int B, int heads, int N, int D, int elem, uintptr_t *lo, uintptr_t *hi);
+// false when two elements may share an address
+bool strides_nest(const long long *s, int B, int heads, int N, int D);
+
 // SM count of the calling thread's current device (looked up once per device); *dev gets its ordinal.
 int current_device_sms(int *dev);
 

@@ -1,0 +1,180 @@
+"""ta_rotary / multi_axis_rotary on the GPU against the formula in 64 bits."""
+import numpy as np
+import pytest
+
+import paper_2410_20926_b200 as ta
+from rotary_reference import angles, coordinates, rotate, tolerance
+
+pytestmark = pytest.mark.gpu
+
+
+def dev(shape, seed, dtype):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn(*shape, device="cuda", generator=gen).to(getattr(torch, dtype))
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def check(x, got, ang, parts, il, dtype, inverse=False):
+    ref = rotate(host(x), ang, parts, il, inverse)
+    tol = tolerance(host(x), ref, ang.shape[-1], parts, il, dtype == "bfloat16")
+    assert (np.abs(host(got) - ref) <= tol).all(), np.abs(host(got) - ref).max()
+
+
+CASES = [  # B, H, H_kv, N, D, parts, sections, ladder per axis
+    (2, 4, 2, 33, 128, 1, (16, 24, 24), False),
+    (1, 8, 2, 64, 128, 2, (10, 12, 10), True),
+    (3, 3, 1, 1, 64, 1, (32,), False),              # one token, one axis
+    (1, 2, 2, 17, 64, 2, (6, 7), True),             # odd pair count, part of the features copied
+    (1, 1, 1, 5, 256, 1, (100, 0, 28), False),      # an axis without pairs, largest head dim
+    (2, 5, 5, 7, 80, 1, (3, 9), False),
+    (1, 3, 1, 9, 13, 1, (2, 4), True),              # odd head dim: rows start at any element
+    (1, 2, 1, 11, 2, 1, (1,), False),               # the smallest head
+    (1, 12, 4, 4, 96, 3, (8, 8), False),
+    (1, 300, 0, 3, 64, 1, (20, 12), False),         # q alone, many heads
+    (1, 40, 8, 9000, 64, 1, (16, 16), False),       # several heads per thread
+    (1, 2, 1, 6, 40, 1, (1, 1, 1, 1, 1, 1, 1, 1), True),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("il", [False, True])
+@pytest.mark.parametrize("case", CASES)
+def test_matches_formula(case, il, dtype):
+    import torch
+    B, H, Hk, N, D, parts, sections, ladder = case
+    q = dev((B, H, N, D), 1, dtype)
+    k = dev((B, Hk, N, D), 2, dtype) if Hk else None
+    rng = np.random.default_rng(5)
+    pos = rng.integers(0, 200000, size=(len(sections), B, N)).astype(np.int32)
+    pos[:, 0, 0] = (2**31 - 1, -2**31, -1, 0)[:len(sections)] + (7,) * max(0, len(sections) - 4)
+    ang = angles(pos.astype(np.int64), sections, 10000.0, ladder)
+    gq, gk = ta.multi_axis_rotary(q, k, sections, positions=torch.from_numpy(pos).cuda(), parts=parts,
+                                  interleaved=il, per_axis_ladder=ladder)
+    check(q, gq, ang, parts, il, dtype)
+    if Hk:
+        check(k, gk, ang, parts, il, dtype)
+    else:
+        assert gk is None
+
+
+@pytest.mark.parametrize("il", [False, True])
+def test_tensor_coordinates_and_offset(il):
+    import torch
+    dims, sections, off, N = (5, 6, 7), (10, 11, 11), 13, 150
+    q, k = dev((2, 4, N, 64), 3, "bfloat16"), dev((2, 2, N, 64), 4, "bfloat16")
+    pos = np.repeat(coordinates(dims, N, off)[:, None, :], 2, 1)
+    ang = angles(pos, sections, 500.0, True)
+    gq, gk = ta.multi_axis_rotary(q, k, sections, dims=dims, token_offset=off, base=500.0, interleaved=il,
+                                  per_axis_ladder=True)
+    check(q, gq, ang, 1, il, "bfloat16")
+    check(k, gk, ang, 1, il, "bfloat16")
+    # the same positions given per token, once for every batch entry
+    p = torch.from_numpy(coordinates(dims, N, off).astype(np.int32)).cuda()
+    hq, hk = ta.multi_axis_rotary(q, k, sections, positions=p, base=500.0, interleaved=il, per_axis_ladder=True)
+    assert torch.equal(gq, hq) and torch.equal(gk, hk)
+    with pytest.raises(ta.TaError):
+        ta.multi_axis_rotary(q, k, sections, dims=dims, token_offset=61)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_strided_and_unaligned_views(dtype):
+    """Views of one fused projection [B, N, (H + 2 H_kv) D], in place through the C ABI, and views off by one element."""
+    import torch
+    B, H, Hk, N, D, sections = 2, 4, 2, 19, 64, (16, 16)
+    pos = np.random.default_rng(6).integers(0, 5000, size=(2, B, N))
+    ang = angles(pos, sections, 10000.0, False)
+    p = torch.from_numpy(pos.astype(np.int32)).cuda()
+    for shift in (0, 1):
+        buf = dev((B, N, (H + 2 * Hk) * D + 8), 7, dtype)
+        rows = buf[..., shift:shift + (H + 2 * Hk) * D].unflatten(-1, (H + 2 * Hk, D)).transpose(1, 2)
+        q, k, v = rows[:, :H], rows[:, H:H + Hk], rows[:, H + Hk:]
+        before = buf.clone()
+        oq, ok = q.clone(), k.clone()
+        gq, gk = ta.multi_axis_rotary(q, k, sections, positions=p)
+        check(oq, gq, ang, 1, False, dtype)
+        check(ok, gk, ang, 1, False, dtype)
+        assert torch.equal(buf, before)
+        st = lambda t: (t.stride(0), t.stride(1), t.stride(2))  # noqa: E731
+        ta.ta_rotary(q, k, q, k, B, H, Hk, N, D, sections, positions=p, q_strides=st(q), k_strides=st(k),
+                     q_out_strides=st(q), k_out_strides=st(k),
+                     dtype=ta.TA_DTYPE_BF16 if dtype == "bfloat16" else ta.TA_DTYPE_F32)
+        assert torch.equal(q, gq) and torch.equal(k, gk)
+        want = before.clone()
+        w = want[..., shift:shift + (H + 2 * Hk) * D].unflatten(-1, (H + 2 * Hk, D)).transpose(1, 2)
+        w[:, :H], w[:, H:H + Hk] = gq, gk
+        assert torch.equal(buf, want)                     # v and everything around the rows as they were
+
+
+def test_broadcast_input_and_transposed_positions():
+    import torch
+    q = dev((1, 1, 6, 64), 8, "float32").expand(3, 4, 6, 64)
+    pos = torch.arange(6 * 3 * 2, dtype=torch.int32, device="cuda").reshape(6, 3, 2).permute(2, 1, 0)
+    gq, _ = ta.multi_axis_rotary(q, None, (8, 8), positions=pos)
+    check(q, gq, angles(pos.cpu().numpy().astype(np.int64), (8, 8), 10000.0, False), 1, False, "float32")
+
+
+def test_copied_features_keep_their_bits():
+    import torch
+    x = dev((1, 2, 5, 64), 9, "bfloat16")
+    x[..., 40:] = float("nan")
+    x[..., 50] = float("inf")
+    for il in (False, True):
+        g, _ = ta.multi_axis_rotary(x, None, (10, 10), dims=(1, 5), interleaved=il)
+        assert torch.equal(g[..., 40:].view(torch.int16), x[..., 40:].view(torch.int16))
+        assert torch.isfinite(g[..., :40]).all()
+
+
+@pytest.mark.parametrize("il", [False, True])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_gradients(il, dtype):
+    import torch
+    B, H, Hk, N, D, sections = 2, 4, 2, 21, 64, (7, 6)
+    q, k = dev((B, H, N, D), 10, dtype).requires_grad_(), dev((B, Hk, N, D), 11, dtype).requires_grad_()
+    pos = np.random.default_rng(12).integers(0, 3000, size=(2, B, N))
+    out = ta.multi_axis_rotary(q, k, sections, positions=torch.from_numpy(pos.astype(np.int32)).cuda(), parts=2, interleaved=il)
+    dq = dev((B, N, H, D), 13, dtype).transpose(1, 2)            # a gradient in another layout
+    dk = dev((B, Hk, N, D), 14, dtype)
+    gq, gk = torch.autograd.grad(out, (q, k), (dq, dk))
+    ang = angles(pos, sections, 10000.0, False)
+    check(dq, gq, ang, 2, il, dtype, inverse=True)
+    check(dk, gk, ang, 2, il, dtype, inverse=True)
+    # against differences: the map is linear, so <rotate(q + e) - rotate(q), g> = <e, grad> up to rounding
+    if dtype == "float32":
+        e = dev((B, H, N, D), 15, dtype)
+        moved, _ = ta.multi_axis_rotary((q + e).detach(), None, sections,
+                                        positions=torch.from_numpy(pos.astype(np.int32)).cuda(), parts=2, interleaved=il)
+        lhs = ((host(moved) - host(out[0])) * host(dq)).sum()
+        rhs = (host(e) * host(gq)).sum()
+        # every term is off by at most 8 steps of 2^-24 of numbers below 8, there are B H N D of them
+        assert abs(lhs - rhs) <= 32 * 2.0 ** -24 * 8 * np.abs(host(dq)).sum()
+
+
+def test_captured_on_another_stream_and_empty():
+    import torch
+    q, k = dev((4, 8, 1, 128), 16, "bfloat16"), dev((4, 2, 1, 128), 17, "bfloat16")
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    pos = torch.randint(0, 1000, (3, 4, 1), device="cuda", dtype=torch.int32)
+    torch.cuda.synchronize()
+
+    def call():
+        ta.ta_rotary(q, k, qo, ko, 4, 8, 2, 1, 128, (16, 24, 24), positions=pos)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        call()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    q.copy_(dev((4, 8, 1, 128), 18, "bfloat16"))
+    pos += 5
+    graph.replay()
+    torch.cuda.synchronize()
+    gq, gk = ta.multi_axis_rotary(q, k, (16, 24, 24), positions=pos)
+    assert torch.equal(gq, qo) and torch.equal(gk, ko)
+    e, f = ta.multi_axis_rotary(q[:0], k[:0], (16, 24, 24), positions=pos[:, :0])
+    assert e.shape == (0, 8, 1, 128) and f.shape == (0, 2, 1, 128)
