@@ -320,11 +320,12 @@ def ta_backward_ex(dout, q, k, v, dq, dk, dv, B, H, H_kv, N, D, dims, causal,
 
 
 def _strides(strides, where):
-    """(batch, head, token) strides in elements as a C array; None: contiguous."""
-    s = (0, 0, 0) if strides is None else [int(x) for x in strides]
-    if len(s) != 3:
+    """(batch, head, token) strides in elements; None: contiguous."""
+    if strides is None:
+        return (0, 0, 0)
+    if len(strides) != 3:
         raise ValueError(f"{where} needs three strides: batch, head, token")
-    return (ctypes.c_longlong * 3)(*s)
+    return tuple(strides)
 
 
 def ta_rotary(q, k, q_out, k_out, B, H, H_kv, N, D, sections, positions=None, pos_axis_stride=None,
@@ -332,24 +333,15 @@ def ta_rotary(q, k, q_out, k_out, B, H, H_kv, N, D, sections, positions=None, po
               per_axis_ladder=False, inverse=False, dtype=TA_DTYPE_BF16, q_strides=None, k_strides=None,
               q_out_strides=None, k_out_strides=None, stream=None, check=True) -> int:
     """Rotary positions with several axes; positions: device int32 [naxes, B, N], or dims (coordinates of the token)."""
-    p = ta_rotary_params()
-    p.struct_bytes = ctypes.sizeof(ta_rotary_params)
-    p.q, p.k, p.q_out, p.k_out = _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out)
-    p.B, p.H, p.H_kv, p.N, p.D = B, H, H_kv, N, D
-    p.dtype, p.parts = dtype, parts
-    p.sections, p.naxes = _dims(sections)
-    p.positions = _ptr(positions)
-    p.pos_axis_stride = B * N if pos_axis_stride is None else pos_axis_stride
-    p.pos_batch_stride = N if pos_batch_stride is None else pos_batch_stride
-    if dims is not None:
-        if len(dims) != len(sections):
-            raise ValueError("dims and sections need one entry per axis")
-        p.dims = _dims(dims)[0]
-    p.token_offset, p.base = token_offset, base
-    p.interleaved, p.per_axis_ladder, p.inverse = int(bool(interleaved)), int(bool(per_axis_ladder)), int(bool(inverse))
-    p.q_strides, p.k_strides = _strides(q_strides, "q"), _strides(k_strides, "k")
-    p.q_out_strides, p.k_out_strides = _strides(q_out_strides, "q_out"), _strides(k_out_strides, "k_out")
-    p.stream = _stream(stream)
+    if dims is not None and len(dims) != len(sections):
+        raise ValueError("dims and sections need one entry per axis")
+    sec, naxes = _dims(sections)
+    p = ta_rotary_params(
+        ctypes.sizeof(ta_rotary_params), _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), B, H, H_kv, N, D, dtype, parts, sec,
+        naxes, _ptr(positions), B * N if pos_axis_stride is None else pos_axis_stride,
+        N if pos_batch_stride is None else pos_batch_stride, None if dims is None else _dims(dims)[0], token_offset, base,
+        int(bool(interleaved)), int(bool(per_axis_ladder)), int(bool(inverse)), _strides(q_strides, "q"),
+        _strides(k_strides, "k"), _strides(q_out_strides, "q_out"), _strides(k_out_strides, "k_out"), _stream(stream))
     return _done(load().ta_rotary(ctypes.byref(p)), "ta_rotary", check)
 
 

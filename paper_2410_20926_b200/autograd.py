@@ -9,6 +9,7 @@ is no fallback.  q: [B, H, N, D]; k, v: [B, H_kv, N, D]; contiguous CUDA tensors
 """
 from __future__ import annotations
 
+import contextlib
 import math
 
 from . import api as ta
@@ -102,8 +103,17 @@ def tensorized_attention(q, k, v, dims, causal=True, softmax_scale=None, rope_ba
                      hop_masks, seq_lens)
 
 
+_SAME_DEVICE = contextlib.nullcontext()
+
+
+def _on(device):
+    """Makes `device` current for a library call (nothing to do when it is)."""
+    import torch
+    return _SAME_DEVICE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
 def _strides3(t):
-    return t.stride(0), t.stride(1), t.stride(2)
+    return t.stride()[:3]
 
 
 def _row_strided(t):
@@ -149,7 +159,7 @@ def _rotary_call(q, k, sections, positions, dims, token_offset, base, parts, int
         batch = positions.stride(1) if positions.dim() == 3 else 0
     if q_out.numel() == 0:
         return q_out, torch.empty_like(k) if k is not None else None
-    with torch.cuda.device(q.device):
+    with _on(q.device):
         ta.ta_rotary(q, k, q_out, k_out, B, H, H_kv, N, D, sections, positions=positions, pos_axis_stride=axis,
                      pos_batch_stride=batch, dims=dims, token_offset=token_offset, base=base, parts=parts,
                      interleaved=interleaved, per_axis_ladder=per_axis_ladder, inverse=inverse,
