@@ -380,6 +380,83 @@ typedef struct ta_rotary_params {
 int ta_rotary(const ta_rotary_params *p);
 
 /*
+ * Differential attention: the difference of two softmax maps over one value tensor,
+ *     out = (A_1 - lambda A_2) V,   A_c = softmax(Q_c K_c^T * scale o M),   Q = [Q_1 | Q_2],  K = [K_1 | K_2],
+ * where Q_1, K_1 are the first D / 2 features of a head and Q_2, K_2 the last, lambda is a learned number per query
+ * head (or one for all), and scale = 1/sqrt(D/2) unless given.  Query head h reads KV head h / (H / H_kv).  One
+ * sequence axis (no tensor dims).
+ *
+ * Nq query rows stand at the END of the keys: with q_lens[b] (Nq without) and kv_lens[b] (Nk without) valid rows and
+ * keys, row t < q_lens[b] has position p = kv_lens[b] - q_lens[b] + t; keys u < kv_lens[b] are visible, with `causal`
+ * those with u <= p.  So Nq == Nk is training or a prompt, Nq == 1 a decoding step against a cache of Nk slots of which
+ * kv_lens[b] are filled, and anything between a chunk of a prompt behind a cache.  A row that sees no key
+ * (kv_lens[b] == 0, or causal with p < 0) and the rows from q_lens[b] on are written as 0 and pass no gradient.  Both
+ * arrays are read on the device in stream order and clamped to [0, Nk] and [0, Nq].  What stands in k and v from
+ * kv_lens[b] on, and in q and dout from q_lens[b] on, does not matter (NaN included).
+ *
+ * bf16 with D = 64 or 128 and 16-byte aligned rows runs on the tensor cores (scores and sums in fp32, weights rounded to
+ * bf16 before the value product); with few query rows (Nq * H / H_kv <= 32) on a kernel that splits the keys over
+ * the GPU.  Everything else -- fp32 (fp32 arithmetic throughout), other even D up to 256, unaligned views,
+ * TA_FLAG_NO_TENSOR_CORE -- runs on CUDA-core kernels.  No atomics: results repeat bit for bit.
+ */
+typedef struct ta_diff_params {
+    size_t struct_bytes;       /* sizeof(ta_diff_params)                                             */
+    const void *q, *k, *v;     /* device: [B,H,Nq,D], [B,H_kv,Nk,D], [B,H_kv,Nk,D]                    */
+    void *out;                 /* device: [B,H,Nq,D]                                                 */
+    const float *lambda;       /* device, lambda_count floats                                        */
+    int lambda_count;          /* H, or 1                                                            */
+    int B, H, H_kv, Nq, Nk, D; /* D even                                                             */
+    int causal;
+    int dtype;                 /* TA_DTYPE_*                                                         */
+    float softmax_scale;       /* 0 -> 1/sqrt(D/2)                                                   */
+    const int *q_lens, *kv_lens; /* DEVICE, B ints, or NULL                                          */
+    long long q_strides[3], k_strides[3], v_strides[3], out_strides[3]; /* elements between batch    */
+                               /* entries, heads, tokens; all 0: contiguous.  D is always innermost   */
+    void *saved;               /* device, 256-byte aligned, TA_DIFF_WS_SAVED bytes, or NULL: what     */
+                               /* ta_diff_backward needs of this pass (row statistics, A_2 V)         */
+    void *workspace;           /* device, 256-byte aligned, TA_DIFF_WS_FORWARD bytes, or NULL: taken  */
+    size_t workspace_bytes;    /* from the library's memory pool in stream order                      */
+    unsigned flags;            /* TA_FLAG_NO_TENSOR_CORE or 0                                        */
+    ta_stream_t stream;
+} ta_diff_params;
+
+int ta_diff_forward(const ta_diff_params *p);
+
+/*
+ * Gradients of differential attention.  With dA = dout V^T, d_c = rowsum(A_c o dA) = <dout, A_c V>:
+ *     dV = (A_1 - lambda A_2)^T dout,   dS_1 = A_1 o (dA - d_1),   dS_2 = -lambda A_2 o (dA - d_2),
+ *     dQ_c = scale dS_c K_c,   dK_c = scale dS_c^T Q_c,   dlambda = -sum(A_2 o dA)
+ * dK, dV summed over the query heads of a group, dlambda[h] over batch entries and rows (over the heads too when
+ * lambda_count is 1).  The maps are recomputed from q, k and the saved statistics.  dq, dk, dv are contiguous and have
+ * the dtype of q; dlambda is fp32.
+ */
+typedef struct ta_diff_bwd_params {
+    size_t struct_bytes;       /* sizeof(ta_diff_bwd_params)                                         */
+    const void *dout, *q, *k, *v, *out; /* device; out: the forward's result                         */
+    const float *lambda;
+    int lambda_count;
+    const void *saved;         /* written by ta_diff_forward with the same arguments                 */
+    void *dq, *dk, *dv;        /* device, contiguous, 16-byte aligned                                */
+    float *dlambda;            /* device, lambda_count floats                                        */
+    int B, H, H_kv, Nq, Nk, D;
+    int causal;
+    int dtype;
+    float softmax_scale;
+    const int *q_lens, *kv_lens;
+    long long dout_strides[3], q_strides[3], k_strides[3], v_strides[3], out_strides[3];
+    void *workspace;           /* device, 256-byte aligned, TA_DIFF_WS_BACKWARD bytes, or NULL        */
+    size_t workspace_bytes;
+    unsigned flags;
+    ta_stream_t stream;
+} ta_diff_bwd_params;
+
+int ta_diff_backward(const ta_diff_bwd_params *p);
+
+/* Bytes of device memory the calls above need for a problem (0 for invalid shapes; the call reports the error). */
+enum { TA_DIFF_WS_FORWARD = 0, TA_DIFF_WS_SAVED = 1, TA_DIFF_WS_BACKWARD = 2 };
+size_t ta_diff_workspace_bytes(int B, int H, int H_kv, int Nq, int Nk, int D, int dtype, int mode);
+
+/*
  * Text description of the launch plan the library would use for a problem (one line per hop:
  * kernel path -- tc, tc-fused, tc-long or simt --, segment length, stride, tile packing,
  * source / destination buffer).  Pure

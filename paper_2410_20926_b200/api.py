@@ -21,12 +21,14 @@ TA_DTYPE_BF16, TA_DTYPE_F32 = 0, 1
 TA_FLAG_NO_TENSOR_CORE, TA_FLAG_NO_HOP_FUSION, TA_FLAG_SAVE_HOPS, TA_FLAG_NO_HOP_OVERLAP = 1, 2, 4, 8
 TA_FLAG_PAIR_HOPS = 16
 TA_FLAG_BF16_INTERMEDIATES = 32
+TA_DIFF_WS_FORWARD, TA_DIFF_WS_SAVED, TA_DIFF_WS_BACKWARD = 0, 1, 2
 TA_WS_FORWARD, TA_WS_FORWARD_SAVE, TA_WS_BACKWARD, TA_WS_BACKWARD_F32_GRADS = 0, 1, 2, 3
 
 EXPORTS = ("ta_forward", "ta_forward_f32", "ta_forward_ex", "ta_backward", "ta_workspace_bytes",
            "ta_forward_host", "ta_plan_describe", "ta_device_status", "ta_launch_count",
            "ta_release", "ta_status_string", "ta_version", "ta_forward_static", "ta_backward_ex",
-           "ta_last_cuda_error", "ta_selftest_wait_timeout", "ta_rotary")
+           "ta_last_cuda_error", "ta_selftest_wait_timeout", "ta_rotary",
+           "ta_diff_forward", "ta_diff_backward", "ta_diff_workspace_bytes")
 TA_STATIC_SCRATCH_BYTES = 16 << 20
 
 
@@ -95,6 +97,45 @@ class ta_rotary_params(ctypes.Structure):
                 ("stream", ctypes.c_void_p)]
 
 
+class ta_diff_params(ctypes.Structure):
+    _fields_ = [("struct_bytes", ctypes.c_size_t),
+                ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("out", ctypes.c_void_p),
+                ("lam", ctypes.c_void_p), ("lambda_count", ctypes.c_int),
+                ("B", ctypes.c_int), ("H", ctypes.c_int), ("H_kv", ctypes.c_int),
+                ("Nq", ctypes.c_int), ("Nk", ctypes.c_int), ("D", ctypes.c_int),
+                ("causal", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("softmax_scale", ctypes.c_float),
+                ("q_lens", ctypes.c_void_p), ("kv_lens", ctypes.c_void_p),
+                ("q_strides", ctypes.c_longlong * 3), ("k_strides", ctypes.c_longlong * 3),
+                ("v_strides", ctypes.c_longlong * 3), ("out_strides", ctypes.c_longlong * 3),
+                ("saved", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+                ("flags", ctypes.c_uint),
+                ("stream", ctypes.c_void_p)]
+
+
+class ta_diff_bwd_params(ctypes.Structure):
+    _fields_ = [("struct_bytes", ctypes.c_size_t),
+                ("dout", ctypes.c_void_p), ("q", ctypes.c_void_p), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("out", ctypes.c_void_p),
+                ("lam", ctypes.c_void_p), ("lambda_count", ctypes.c_int),
+                ("saved", ctypes.c_void_p),
+                ("dq", ctypes.c_void_p), ("dk", ctypes.c_void_p), ("dv", ctypes.c_void_p),
+                ("dlambda", ctypes.c_void_p),
+                ("B", ctypes.c_int), ("H", ctypes.c_int), ("H_kv", ctypes.c_int),
+                ("Nq", ctypes.c_int), ("Nk", ctypes.c_int), ("D", ctypes.c_int),
+                ("causal", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("softmax_scale", ctypes.c_float),
+                ("q_lens", ctypes.c_void_p), ("kv_lens", ctypes.c_void_p),
+                ("dout_strides", ctypes.c_longlong * 3), ("q_strides", ctypes.c_longlong * 3),
+                ("k_strides", ctypes.c_longlong * 3), ("v_strides", ctypes.c_longlong * 3),
+                ("out_strides", ctypes.c_longlong * 3),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+                ("flags", ctypes.c_uint),
+                ("stream", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -133,6 +174,10 @@ def load():
     lib.ta_last_cuda_error.restype = ctypes.c_int
     lib.ta_version.argtypes = []
     lib.ta_rotary.argtypes = [ctypes.POINTER(ta_rotary_params)]
+    lib.ta_diff_forward.argtypes = [ctypes.POINTER(ta_diff_params)]
+    lib.ta_diff_backward.argtypes = [ctypes.POINTER(ta_diff_bwd_params)]
+    lib.ta_diff_workspace_bytes.argtypes = [ci] * 8
+    lib.ta_diff_workspace_bytes.restype = ctypes.c_size_t
     for name in EXPORTS:
         getattr(lib, name)          # every symbol of include/ta.h must be exported
     _lib = lib
@@ -343,6 +388,37 @@ def ta_rotary(q, k, q_out, k_out, B, H, H_kv, N, D, sections, positions=None, po
         int(bool(interleaved)), int(bool(per_axis_ladder)), int(bool(inverse)), _strides(q_strides, "q"),
         _strides(k_strides, "k"), _strides(q_out_strides, "q_out"), _strides(k_out_strides, "k_out"), _stream(stream))
     return _done(load().ta_rotary(ctypes.byref(p)), "ta_rotary", check)
+
+
+def ta_diff_forward(q, k, v, out, lam, lambda_count, B, H, H_kv, Nq, Nk, D, causal, dtype=TA_DTYPE_BF16,
+                    softmax_scale=0.0, q_lens=None, kv_lens=None, q_strides=None, k_strides=None, v_strides=None,
+                    out_strides=None, saved=None, workspace=None, workspace_bytes=0, flags=0, stream=None,
+                    check=True) -> int:
+    """Differential attention; lam: device float32 [lambda_count], lambda_count H or 1."""
+    p = ta_diff_params(
+        ctypes.sizeof(ta_diff_params), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lam), lambda_count, B, H, H_kv, Nq, Nk,
+        D, int(bool(causal)), dtype, softmax_scale, _ptr(q_lens), _ptr(kv_lens), _strides(q_strides, "q"),
+        _strides(k_strides, "k"), _strides(v_strides, "v"), _strides(out_strides, "out"), _ptr(saved), _ptr(workspace),
+        workspace_bytes, flags, _stream(stream))
+    return _done(load().ta_diff_forward(ctypes.byref(p)), "ta_diff_forward", check)
+
+
+def ta_diff_backward(dout, q, k, v, out, lam, lambda_count, saved, dq, dk, dv, dlambda, B, H, H_kv, Nq, Nk, D, causal,
+                     dtype=TA_DTYPE_BF16, softmax_scale=0.0, q_lens=None, kv_lens=None, dout_strides=None,
+                     q_strides=None, k_strides=None, v_strides=None, out_strides=None, workspace=None,
+                     workspace_bytes=0, flags=0, stream=None, check=True) -> int:
+    """Gradients of ta_diff_forward from what it left in `saved`; dq, dk, dv contiguous, dlambda float32."""
+    p = ta_diff_bwd_params(
+        ctypes.sizeof(ta_diff_bwd_params), _ptr(dout), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lam), lambda_count,
+        _ptr(saved), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dlambda), B, H, H_kv, Nq, Nk, D, int(bool(causal)), dtype,
+        softmax_scale, _ptr(q_lens), _ptr(kv_lens), _strides(dout_strides, "dout"), _strides(q_strides, "q"),
+        _strides(k_strides, "k"), _strides(v_strides, "v"), _strides(out_strides, "out"), _ptr(workspace),
+        workspace_bytes, flags, _stream(stream))
+    return _done(load().ta_diff_backward(ctypes.byref(p)), "ta_diff_backward", check)
+
+
+def ta_diff_workspace_bytes(B, H, H_kv, Nq, Nk, D, dtype=TA_DTYPE_BF16, mode=TA_DIFF_WS_FORWARD) -> int:
+    return int(load().ta_diff_workspace_bytes(B, H, H_kv, Nq, Nk, D, dtype, mode))
 
 
 def ta_workspace_bytes(B, H, H_kv, N, D, dims, dtype=TA_DTYPE_BF16, mode=TA_WS_FORWARD) -> int:

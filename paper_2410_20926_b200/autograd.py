@@ -1,5 +1,5 @@
-"""torch.autograd binding of the C-ABI library: ``tensorized_attention(q, k, v, dims, ...)`` and
-``multi_axis_rotary(q, k, sections, ...)``.
+"""torch.autograd binding of the C-ABI library: ``tensorized_attention(q, k, v, dims, ...)``,
+``multi_axis_rotary(q, k, sections, ...)`` and ``differential_attention(q, k, v, lam, ...)``.
 
 Marshalling only.  The forward is ``ta_forward_ex`` (with ``TA_FLAG_SAVE_HOPS`` when a gradient is
 needed, so the hop inputs X_1..X_{m-1} are kept instead of recomputed), the backward is
@@ -210,3 +210,104 @@ def multi_axis_rotary(q, k, sections, positions=None, dims=None, token_offset=0,
     if _ROTARY is None:
         _ROTARY = _rotary_function()
     return _ROTARY.apply(q, k, positions, args)
+
+
+def _check_diff(q, k, v, lam, q_lens, kv_lens):
+    import torch
+    if not q.is_cuda or any(t.device != q.device for t in (k, v, lam)):
+        raise ValueError("differential_attention needs CUDA tensors on one device (there is no CPU path)")
+    if q.dim() != 4 or k.dim() != 4 or v.shape != k.shape:
+        raise ValueError("expected q [B,H,Nq,D] and k, v [B,H_kv,Nk,D]")
+    B, H, Nq, D = q.shape
+    if k.shape[0] != B or k.shape[3] != D:
+        raise ValueError("q and k, v disagree in batch or head dim")
+    if q.dtype not in (torch.bfloat16, torch.float32) or k.dtype != q.dtype or v.dtype != q.dtype:
+        raise ValueError("q, k, v must all be bfloat16 or all float32")
+    if q.numel() == 0 or k.numel() == 0:
+        raise ValueError("differential_attention needs at least one query row and one key slot")
+    if lam.dtype != torch.float32 or lam.numel() not in (1, H) or lam.dim() > 1:
+        raise ValueError("lam must hold H float32 numbers, or one")
+    for t in (q_lens, kv_lens):
+        if t is not None and (t.dtype != torch.int32 or t.device != q.device or t.dim() != 1 or t.numel() != B
+                              or not t.is_contiguous()):
+            raise ValueError("q_lens and kv_lens must be int32 [B], contiguous, on the device of q")
+    return B, H, k.shape[1], Nq, k.shape[2], D
+
+
+def _diff_forward(q, k, v, lam, causal, softmax_scale, q_lens, kv_lens, save):
+    import torch
+    B, H, H_kv, Nq, Nk, D = q.shape[0], q.shape[1], k.shape[1], q.shape[2], k.shape[2], q.shape[3]
+    dtype = ta.TA_DTYPE_BF16 if q.dtype == torch.bfloat16 else ta.TA_DTYPE_F32
+    out = torch.empty((B, H, Nq, D), dtype=q.dtype, device=q.device)
+    saved = None
+    with _on(q.device):
+        if save:
+            saved = torch.empty(ta.ta_diff_workspace_bytes(B, H, H_kv, Nq, Nk, D, dtype, ta.TA_DIFF_WS_SAVED),
+                                dtype=torch.uint8, device=q.device)
+        nbytes = ta.ta_diff_workspace_bytes(B, H, H_kv, Nq, Nk, D, dtype, ta.TA_DIFF_WS_FORWARD)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=q.device) if nbytes else None
+        ta.ta_diff_forward(q, k, v, out, lam, lam.numel(), B, H, H_kv, Nq, Nk, D, causal, dtype=dtype,
+                           softmax_scale=softmax_scale or 0.0, q_lens=q_lens, kv_lens=kv_lens, q_strides=_strides3(q),
+                           k_strides=_strides3(k), v_strides=_strides3(v), saved=saved, workspace=ws,
+                           workspace_bytes=nbytes)
+    return out, saved
+
+
+_DIFF = None
+
+
+def _diff_function():
+    import torch
+
+    class _DifferentialAttention(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, v, lam, causal, softmax_scale, q_lens, kv_lens):
+            q, k, v, lam = _row_strided(q), _row_strided(k), _row_strided(v), lam.contiguous()
+            save = any(ctx.needs_input_grad[:4])
+            out, saved = _diff_forward(q, k, v, lam, causal, softmax_scale, q_lens, kv_lens, save)
+            if save:
+                ctx.save_for_backward(q, k, v, lam, out, saved, q_lens, kv_lens)
+                ctx.args = (causal, softmax_scale)
+            return out
+
+        @staticmethod
+        def backward(ctx, dout):
+            q, k, v, lam, out, saved, q_lens, kv_lens = ctx.saved_tensors
+            causal, softmax_scale = ctx.args
+            B, H, H_kv, Nq, Nk, D = q.shape[0], q.shape[1], k.shape[1], q.shape[2], k.shape[2], q.shape[3]
+            dtype = ta.TA_DTYPE_BF16 if q.dtype == torch.bfloat16 else ta.TA_DTYPE_F32
+            dout = dout.contiguous()
+            dq = torch.empty((B, H, Nq, D), dtype=q.dtype, device=q.device)
+            dk = torch.empty((B, H_kv, Nk, D), dtype=q.dtype, device=q.device)
+            dv = torch.empty_like(dk)
+            dlam = torch.empty(lam.shape, dtype=torch.float32, device=q.device)
+            with _on(q.device):
+                nbytes = ta.ta_diff_workspace_bytes(B, H, H_kv, Nq, Nk, D, dtype, ta.TA_DIFF_WS_BACKWARD)
+                ws = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+                ta.ta_diff_backward(dout, q, k, v, out, lam, lam.numel(), saved, dq, dk, dv, dlam, B, H, H_kv, Nq, Nk, D,
+                                    causal, dtype=dtype, softmax_scale=softmax_scale or 0.0, q_lens=q_lens,
+                                    kv_lens=kv_lens, dout_strides=_strides3(dout), q_strides=_strides3(q),
+                                    k_strides=_strides3(k), v_strides=_strides3(v), workspace=ws,
+                                    workspace_bytes=nbytes)
+            return dq, dk, dv, dlam, None, None, None, None
+
+    return _DifferentialAttention
+
+
+def differential_attention(q, k, v, lam, causal=True, softmax_scale=None, q_lens=None, kv_lens=None):
+    """(softmax(Q1 K1^T s) - lam softmax(Q2 K2^T s)) V, differentiable with respect to q, k, v and lam.
+
+    q: [B, H, Nq, D] = [Q1 | Q2]; k: [B, H_kv, Nk, D] = [K1 | K2]; v: [B, H_kv, Nk, D]; all bfloat16 or all float32, D
+    even, innermost features adjacent (other strides are free).  lam: float32, one number per query head or one for all.
+    s: 1/sqrt(D/2) unless given.  The query rows stand at the end of the keys: row t has position
+    kv_lens[b] - q_lens[b] + t and, with `causal`, sees the keys up to it; q_lens, kv_lens: int32 CUDA tensors [B] of
+    valid rows and keys (all of them by default).  Rows that see nothing are 0.  Returns [B, H, Nq, D], contiguous.
+    """
+    global _DIFF
+    _check_diff(q, k, v, lam, q_lens, kv_lens)
+    if not (q.requires_grad or k.requires_grad or v.requires_grad or lam.requires_grad):
+        return _diff_forward(_row_strided(q), _row_strided(k), _row_strided(v), lam.contiguous(), bool(causal),
+                             softmax_scale, q_lens, kv_lens, False)[0]
+    if _DIFF is None:
+        _DIFF = _diff_function()
+    return _DIFF.apply(q, k, v, lam, bool(causal), softmax_scale, q_lens, kv_lens)

@@ -1,0 +1,268 @@
+// Differential attention: argument checks, buffers and the choice of kernels (ta_diff_forward, ta_diff_backward,
+// ta_diff_workspace_bytes).
+#include <math.h>
+
+#include "ta_diff.h"
+
+namespace ta {
+namespace {
+
+size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Query rows of a GQA group up to which the keys are split over blocks that each take all of them.
+constexpr int kSplitRows = 32;
+
+// Head dims and group sizes as the calls check them; TA_OK or the error.
+int check_shape(int B, int H, int H_kv, int Nq, int Nk, int D, int dtype) {
+    if (B < 1 || H < 1 || H_kv < 1 || Nq < 1 || Nk < 1 || D < 1) return TA_ERR_INVALID_ARG;
+    if (H % H_kv) return TA_ERR_SHAPE;
+    if (dtype != TA_DTYPE_BF16 && dtype != TA_DTYPE_F32) return TA_ERR_UNSUPPORTED;
+    if (D > TA_MAX_HEAD_DIM || (D & 1)) return TA_ERR_UNSUPPORTED;
+    // rows and tokens are counted in 32 bits, elements in 64
+    if ((long long)B * H > 0x7FFFFFFFll / kDiffRowPad || (long long)B * H * diff_padded_rows(Nq) > (1ll << 40) ||
+        (long long)B * H_kv * Nk > (1ll << 40) || Nq > 0x7FFFFF00 || Nk > 0x7FFFFF00)
+        return TA_ERR_TOO_LARGE;
+    return TA_OK;
+}
+
+bool few_rows(int H, int H_kv, int Nq) { return (long long)(H / H_kv) * Nq <= kSplitRows; }
+
+// Key ranges of the split kernels: about four blocks per SM, ranges of 256 keys or more.
+int num_splits(int B, int H, int H_kv, int Nq, int Nk) {
+    const long long rows = (long long)(H / H_kv) * Nq, groups = (rows + 7) / 8;
+    const long long blocks = (long long)B * H_kv * groups;
+    const long long want = 4ll * current_device_sms(nullptr);
+    long long s = (want + blocks - 1) / blocks;
+    const long long most = ((long long)Nk + 255) / 256;
+    if (s > most) s = most;
+    if (s > 256) s = 256;
+    return s < 1 ? 1 : (int)s;
+}
+
+// Head chunks of a GQA group whose dK, dV partials are kept apart: the group is split while its items are fewer than
+// four per SM.
+int head_chunks(int B, int H, int H_kv, int Nk, int tile) {
+    const int g = H / H_kv;
+    const long long blocks = (long long)B * H_kv * ((Nk + tile - 1) / tile);
+    int s = 1;
+    for (int d = 2; d <= g && blocks * s < 4ll * current_device_sms(nullptr); ++d)
+        if (g % d == 0) s = d;
+    return s;
+}
+
+struct SavedLayout {
+    size_t lse, o2, total;
+};
+SavedLayout saved_layout(int B, int H, int Nq, int D, int dtype) {
+    SavedLayout L;
+    L.lse = 0;
+    L.o2 = up256((size_t)B * H * Nq * sizeof(float2));
+    L.total = L.o2 + up256((size_t)B * H * Nq * D * elem_bytes(dtype));
+    return L;
+}
+
+size_t forward_bytes(int B, int H, int H_kv, int Nq, int Nk, int D) {
+    if (!few_rows(H, H_kv, Nq)) return 0;
+    const size_t slots = (size_t)B * H * Nq * num_splits(B, H, H_kv, Nq, Nk);
+    return up256(slots * sizeof(float4)) + up256(slots * 2 * D * sizeof(float));
+}
+
+struct BackwardLayout {
+    size_t stats, dlam, part, total;
+    int q_tile, k_tile, hsplit;
+};
+BackwardLayout backward_layout(int B, int H, int H_kv, int Nq, int Nk, int D, bool tc) {
+    BackwardLayout L;
+    L.q_tile = L.k_tile = diff_simt_tile(D);
+    (void)tc;
+    L.hsplit = head_chunks(B, H, H_kv, Nk, L.k_tile);
+    L.stats = 0;
+    L.dlam = up256((size_t)B * H * diff_padded_rows(Nq) * sizeof(float4));
+    L.part = L.dlam + up256((size_t)B * H * ((Nq + L.q_tile - 1) / L.q_tile) * sizeof(float));
+    L.total = L.part + (L.hsplit > 1 ? up256((size_t)2 * L.hsplit * B * H_kv * Nk * D * sizeof(float)) : 0);
+    return L;
+}
+
+Strides3 strides_of(const long long *given, int heads, int N, int D) {
+    long long s[3];
+    take_strides(given, heads, N, D, s);
+    return {s[0], s[1], s[2]};
+}
+
+struct Tensor {
+    const void *p;
+    const long long *strides;
+    int heads, N;
+    bool written;
+};
+
+// every address on an element boundary; nothing that is written shares memory with anything else
+int check_tensors(const Tensor *t, int n, int B, int D, int elem) {
+    for (int i = 0; i < n; ++i) {
+        if ((uintptr_t)t[i].p % elem) return TA_ERR_ALIGNMENT;
+        long long s[3];
+        take_strides(t[i].strides, t[i].heads, t[i].N, D, s);
+        if (t[i].written && !strides_nest(s, B, t[i].heads, t[i].N, D)) return TA_ERR_INVALID_ARG;
+    }
+    auto dense = [&](const Tensor &x) {
+        long long s[3];
+        take_strides(x.strides, x.heads, x.N, D, s);
+        return (s[2] == D || x.N == 1) && (s[1] == (long long)x.N * D || x.heads == 1) && (s[0] == (long long)x.heads * x.N * D || B == 1);
+    };
+    for (int i = 0; i < n; ++i)
+        for (int j = 0; j < n; ++j) {
+            if (i == j || !t[i].written) continue;
+            if (t[i].p == t[j].p) return TA_ERR_INVALID_ARG;
+            // views of one buffer span one another without sharing an element: only tensors without gaps are compared
+            if (!dense(t[i]) || !dense(t[j])) continue;
+            uintptr_t lo, hi, l2, h2;
+            long long s[3];
+            take_strides(t[i].strides, t[i].heads, t[i].N, D, s);
+            strided_extent(t[i].p, s, B, t[i].heads, t[i].N, D, elem, &lo, &hi);
+            take_strides(t[j].strides, t[j].heads, t[j].N, D, s);
+            strided_extent(t[j].p, s, B, t[j].heads, t[j].N, D, elem, &l2, &h2);
+            if (lo < h2 && l2 < hi) return TA_ERR_INVALID_ARG;
+        }
+    return TA_OK;
+}
+
+int check_common(const float *lambda, int lambda_count, int H, float scale, unsigned flags, const void *ws) {
+    if (!lambda || (lambda_count != 1 && lambda_count != H)) return TA_ERR_INVALID_ARG;
+    if (!isfinite(scale)) return TA_ERR_INVALID_ARG;
+    if (flags & ~(unsigned)TA_FLAG_NO_TENSOR_CORE) return TA_ERR_UNSUPPORTED;
+    if ((uintptr_t)lambda % 4 || (uintptr_t)ws % 256) return TA_ERR_ALIGNMENT;
+    return TA_OK;
+}
+
+const long long kContiguous[3] = {0, 0, 0};
+
+int forward_impl(const ta_diff_params &p) {
+    if (!p.q || !p.k || !p.v || !p.out) return TA_ERR_INVALID_ARG;
+    int rc = check_shape(p.B, p.H, p.H_kv, p.Nq, p.Nk, p.D, p.dtype);
+    if (rc != TA_OK) return rc;
+    if ((rc = check_common(p.lambda, p.lambda_count, p.H, p.softmax_scale, p.flags, p.workspace)) != TA_OK) return rc;
+    if ((uintptr_t)p.saved % 256) return TA_ERR_ALIGNMENT;
+    const int elem = (int)elem_bytes(p.dtype);
+    const Tensor t[4] = {{p.q, p.q_strides, p.H, p.Nq, false}, {p.k, p.k_strides, p.H_kv, p.Nk, false},
+                         {p.v, p.v_strides, p.H_kv, p.Nk, false}, {p.out, p.out_strides, p.H, p.Nq, true}};
+    if ((rc = check_tensors(t, 4, p.B, p.D, elem)) != TA_OK) return rc;
+    const size_t need = forward_bytes(p.B, p.H, p.H_kv, p.Nq, p.Nk, p.D);
+    if (p.workspace && p.workspace_bytes < need) return TA_ERR_WORKSPACE;
+    if ((rc = check_arch()) != TA_OK) return rc;
+
+    DiffProblem d = {};
+    d.q = p.q; d.k = p.k; d.v = p.v; d.out = p.out;
+    d.sq = strides_of(p.q_strides, p.H, p.Nq, p.D);
+    d.sk = strides_of(p.k_strides, p.H_kv, p.Nk, p.D);
+    d.sv = strides_of(p.v_strides, p.H_kv, p.Nk, p.D);
+    d.so = strides_of(p.out_strides, p.H, p.Nq, p.D);
+    d.lambda = p.lambda; d.lambda_count = p.lambda_count;
+    d.B = p.B; d.H = p.H; d.H_kv = p.H_kv; d.Nq = p.Nq; d.Nk = p.Nk; d.D = p.D;
+    d.causal = p.causal ? 1 : 0; d.dtype = p.dtype;
+    d.scale = p.softmax_scale != 0.f ? p.softmax_scale : 1.0f / sqrtf((float)(p.D / 2));
+    d.q_lens = p.q_lens; d.kv_lens = p.kv_lens;
+    if (p.saved) {
+        const SavedLayout L = saved_layout(p.B, p.H, p.Nq, p.D, p.dtype);
+        d.lse = (float2 *)((char *)p.saved + L.lse);
+        d.o2 = (char *)p.saved + L.o2;
+    }
+    d.stream = (cudaStream_t)p.stream;
+    if (!few_rows(p.H, p.H_kv, p.Nq)) return launch_diff_simt(d);
+    char *ws = (char *)p.workspace;
+    PooledGuard pooled{nullptr, d.stream};
+    if (!ws) {
+        if ((rc = pool_alloc(need, d.stream, &pooled.ptr)) != TA_OK) return rc;
+        ws = (char *)pooled.ptr;
+    }
+    DiffPartials part;
+    part.splits = num_splits(p.B, p.H, p.H_kv, p.Nq, p.Nk);
+    part.ml = (float4 *)ws;
+    part.acc = (float *)(ws + up256((size_t)p.B * p.H * p.Nq * part.splits * sizeof(float4)));
+    if ((rc = launch_diff_simt_split(d, part)) != TA_OK) return rc;
+    return launch_diff_combine(d, part);
+}
+
+int backward_impl(const ta_diff_bwd_params &p) {
+    if (!p.dout || !p.q || !p.k || !p.v || !p.out || !p.saved || !p.dq || !p.dk || !p.dv || !p.dlambda) return TA_ERR_INVALID_ARG;
+    int rc = check_shape(p.B, p.H, p.H_kv, p.Nq, p.Nk, p.D, p.dtype);
+    if (rc != TA_OK) return rc;
+    if ((rc = check_common(p.lambda, p.lambda_count, p.H, p.softmax_scale, p.flags, p.workspace)) != TA_OK) return rc;
+    if ((uintptr_t)p.saved % 256 || (uintptr_t)p.dlambda % 4 || (uintptr_t)p.dq % 16 || (uintptr_t)p.dk % 16 || (uintptr_t)p.dv % 16)
+        return TA_ERR_ALIGNMENT;
+    const int elem = (int)elem_bytes(p.dtype);
+    const Tensor t[8] = {{p.q, p.q_strides, p.H, p.Nq, false}, {p.k, p.k_strides, p.H_kv, p.Nk, false},
+                         {p.v, p.v_strides, p.H_kv, p.Nk, false}, {p.out, p.out_strides, p.H, p.Nq, false},
+                         {p.dout, p.dout_strides, p.H, p.Nq, false}, {p.dq, kContiguous, p.H, p.Nq, true},
+                         {p.dk, kContiguous, p.H_kv, p.Nk, true}, {p.dv, kContiguous, p.H_kv, p.Nk, true}};
+    if ((rc = check_tensors(t, 8, p.B, p.D, elem)) != TA_OK) return rc;
+    const BackwardLayout L = backward_layout(p.B, p.H, p.H_kv, p.Nq, p.Nk, p.D, false);
+    if (p.workspace && p.workspace_bytes < L.total) return TA_ERR_WORKSPACE;
+    if ((rc = check_arch()) != TA_OK) return rc;
+
+    DiffProblem d = {};
+    d.q = p.q; d.k = p.k; d.v = p.v; d.out = const_cast<void *>(p.out); d.dout = p.dout;
+    d.sq = strides_of(p.q_strides, p.H, p.Nq, p.D);
+    d.sk = strides_of(p.k_strides, p.H_kv, p.Nk, p.D);
+    d.sv = strides_of(p.v_strides, p.H_kv, p.Nk, p.D);
+    d.so = strides_of(p.out_strides, p.H, p.Nq, p.D);
+    d.sdo = strides_of(p.dout_strides, p.H, p.Nq, p.D);
+    d.lambda = p.lambda; d.lambda_count = p.lambda_count;
+    d.B = p.B; d.H = p.H; d.H_kv = p.H_kv; d.Nq = p.Nq; d.Nk = p.Nk; d.D = p.D;
+    d.causal = p.causal ? 1 : 0; d.dtype = p.dtype;
+    d.scale = p.softmax_scale != 0.f ? p.softmax_scale : 1.0f / sqrtf((float)(p.D / 2));
+    d.q_lens = p.q_lens; d.kv_lens = p.kv_lens;
+    const SavedLayout S = saved_layout(p.B, p.H, p.Nq, p.D, p.dtype);
+    d.lse = (float2 *)((char *)const_cast<void *>(p.saved) + S.lse);
+    d.o2 = (char *)const_cast<void *>(p.saved) + S.o2;
+    d.stream = (cudaStream_t)p.stream;
+    char *ws = (char *)p.workspace;
+    PooledGuard pooled{nullptr, d.stream};
+    if (!ws) {
+        if ((rc = pool_alloc(L.total, d.stream, &pooled.ptr)) != TA_OK) return rc;
+        ws = (char *)pooled.ptr;
+    }
+    DiffGrads g = {};
+    g.stats = (const float4 *)(ws + L.stats);
+    g.dq = p.dq; g.dk = p.dk; g.dv = p.dv;
+    g.part = (float *)(ws + L.part);
+    g.hsplit = L.hsplit;
+    g.dlam_part = (float *)(ws + L.dlam);
+    if ((rc = launch_diff_stats(d, (float4 *)(ws + L.stats))) != TA_OK) return rc;
+    if ((rc = launch_diff_simt_bwd(d, g)) != TA_OK) return rc;
+    if (g.hsplit > 1 && (rc = launch_diff_group_sum(d, g)) != TA_OK) return rc;
+    return launch_diff_dlambda(d, g, (p.Nq + L.q_tile - 1) / L.q_tile, p.dlambda);
+}
+
+int finish(int rc) {
+    if (rc == TA_ERR_CUDA && tl_last_cuda_error == 0) tl_last_cuda_error = (int)cudaPeekAtLastError();
+    return rc;
+}
+
+}  // namespace
+}  // namespace ta
+
+using namespace ta;
+
+extern "C" {
+
+int ta_diff_forward(const ta_diff_params *p) {
+    if (!p || p->struct_bytes != sizeof(ta_diff_params)) return TA_ERR_INVALID_ARG;
+    tl_last_cuda_error = 0;
+    return finish(forward_impl(*p));
+}
+
+int ta_diff_backward(const ta_diff_bwd_params *p) {
+    if (!p || p->struct_bytes != sizeof(ta_diff_bwd_params)) return TA_ERR_INVALID_ARG;
+    tl_last_cuda_error = 0;
+    return finish(backward_impl(*p));
+}
+
+size_t ta_diff_workspace_bytes(int B, int H, int H_kv, int Nq, int Nk, int D, int dtype, int mode) {
+    if (check_shape(B, H, H_kv, Nq, Nk, D, dtype) != TA_OK) return 0;
+    if (mode == TA_DIFF_WS_FORWARD) return forward_bytes(B, H, H_kv, Nq, Nk, D);
+    if (mode == TA_DIFF_WS_SAVED) return saved_layout(B, H, Nq, D, dtype).total;
+    if (mode == TA_DIFF_WS_BACKWARD) return backward_layout(B, H, H_kv, Nq, Nk, D, false).total;
+    return 0;
+}
+
+}  // extern "C"

@@ -1,0 +1,78 @@
+// Differential attention, shared by its translation units: the resolved problem, the spans of a batch entry, and the
+// launchers of the kernels (ta_diff.cu: argument checks, buffers, dispatch).
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "ta_internal.h"
+
+namespace ta {
+
+struct Strides3 {
+    long long b, h, n;   // elements between batch entries, heads, tokens
+};
+
+struct DiffProblem {
+    const void *q, *k, *v;
+    void *out;                   // forward: written; backward: the forward's result, read
+    const void *dout;
+    Strides3 sq, sk, sv, so, sdo;
+    const float *lambda;
+    int lambda_count;
+    int B, H, H_kv, Nq, Nk, D, causal, dtype;
+    float scale;
+    const int *q_lens, *kv_lens;
+    float2 *lse;                 // [B*H*Nq]: log2 of the sum of 2^(score * scale * log2 e), per map; +inf: row sees no key
+    void *o2;                    // [B,H,Nq,D] contiguous: A_2 V, dtype
+    cudaStream_t stream;
+};
+
+// Valid rows and keys of batch entry b; row t stands at key position t + off.
+struct DiffSpan {
+    int ql, kl, off;
+    // keys row t sees: [0, keys(t))
+    __device__ __forceinline__ int keys(int t, int causal) const {
+        if (t >= ql) return 0;
+        return causal ? max(0, min(kl, t + off + 1)) : kl;
+    }
+};
+__device__ __forceinline__ DiffSpan diff_span(const int *q_lens, const int *kv_lens, int b, int Nq, int Nk) {
+    DiffSpan s;
+    s.ql = q_lens ? min(max(__ldg(q_lens + b), 0), Nq) : Nq;
+    s.kl = kv_lens ? min(max(__ldg(kv_lens + b), 0), Nk) : Nk;
+    s.off = s.kl - s.ql;
+    return s;
+}
+
+// Buffers of one call behind the forward's workspace: partial results of `splits` key ranges per query row,
+// [row][split]: (m_1, l_1, m_2, l_2) and the two un-normalised value sums, D floats each.
+struct DiffPartials {
+    float4 *ml;
+    float *acc;
+    int splits;
+};
+
+// Row statistics of the backward, [B*H][rows padded to 128]: (lse_1, lse_2, d_1, d_2); rows without a visible key and
+// the padding hold (+inf, +inf, 0, 0), so that their weights come out as 0.
+constexpr int kDiffRowPad = 128;
+inline long long diff_padded_rows(int Nq) { return ((long long)Nq + kDiffRowPad - 1) / kDiffRowPad * kDiffRowPad; }
+
+struct DiffGrads {
+    const float4 *stats;
+    void *dq, *dk, *dv;          // contiguous, dtype
+    float *part;                 // dK, dV partials [2][hsplit][B*H_kv*Nk*D] when hsplit > 1
+    int hsplit;                  // items a GQA group's query heads are split over
+    float *dlam_part;            // [B*H][q tiles of the kernel in use]: sums of A_2 o dA
+};
+
+// generic CUDA-core kernels (ta_diff_simt.cu)
+int diff_simt_tile(int D);                       // rows of a query tile / key tile
+int launch_diff_simt(const DiffProblem &p);
+int launch_diff_simt_split(const DiffProblem &p, const DiffPartials &part);
+int launch_diff_combine(const DiffProblem &p, const DiffPartials &part);
+int launch_diff_stats(const DiffProblem &p, float4 *stats);
+int launch_diff_simt_bwd(const DiffProblem &p, const DiffGrads &g);
+int launch_diff_group_sum(const DiffProblem &p, const DiffGrads &g);
+int launch_diff_dlambda(const DiffProblem &p, const DiffGrads &g, int tiles, float *dlambda);
+
+}  // namespace ta

@@ -1,0 +1,826 @@
+// Differential attention on CUDA cores: fp32 arithmetic throughout, any even head dim up to 256, fp32 or bf16 storage.
+//
+//     out = (A_1 - lambda A_2) V,   A_c = softmax(Q_c K_c^T scale o M)
+//
+// Forward (tile kernel): one block per tile of query rows; key tiles go by once, both maps keep a running maximum and
+// sum, the two value sums stay in registers until the end, where they are normalised and subtracted.  16 x 16 threads
+// hold square micro-tiles of both score maps (4 x 4, or 2 x 2 above head dim 128), operands in shared memory; K and V
+// share one buffer so that two blocks fit an SM at head dim 128.
+// Forward (split kernel, few query rows): one block per (KV head, up to 8 query rows, key range); the rows of a GQA
+// group share the K / V tiles it loads.  Its partial sums meet in the combine kernel.
+// Backward: two passes that recompute the maps -- one block per query tile for dQ and the sum for dlambda, one per key
+// tile for dK and dV -- so that every sum is taken in one place in one order and nothing is added atomically.
+#include <math.h>
+
+#include "ta_diff.h"
+#include "ta_ptx.cuh"
+
+namespace ta {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float load1(const float *p) { return __ldg(p); }
+__device__ __forceinline__ float load1(const __nv_bfloat16 *p) { return __bfloat162float(__ldg(p)); }
+__device__ __forceinline__ void store1(float *p, float x) { *p = x; }
+__device__ __forceinline__ void store1(__nv_bfloat16 *p, float x) { *p = __float2bfloat16_rn(x); }
+
+template <int DT>
+struct Tile {
+    static constexpr int kRows = DT > 128 ? 32 : 64;   // query rows = keys of a tile
+    static constexpr int kM = kRows / 16;              // micro-tile edge
+    static constexpr int kLd = DT + 4;                 // floats per operand row (16-byte aligned, conflict-free)
+    static constexpr int kLp = kRows + 4;              // floats per row of a weight tile
+    static constexpr int kCh = DT / 64;                // 4-column chunks per thread of a rows x DT product
+};
+
+// rows [r0, r0 + kRows) of a strided matrix into shared memory as floats; the two halves of the head dim go to columns
+// 0 and DT / 2; rows from `valid` on and the columns between the halves are 0
+template <typename T, int DT>
+__device__ __forceinline__ void load_tile(float *dst, const T *src, long long stride, int r0, int valid, int D) {
+    using C = Tile<DT>;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = D >> 1;
+    for (int r = warp; r < C::kRows; r += kThreads / 32) {
+        const bool in = r0 + r < valid;
+        const T *row = src + (long long)(r0 + r) * stride;
+        for (int c = lane; c < DT; c += 32) {
+            const int hi = c >= DT / 2 ? 1 : 0, cc = c - hi * (DT / 2);
+            dst[r * C::kLd + c] = (in && cc < half) ? load1(row + hi * half + cc) : 0.f;
+        }
+    }
+}
+
+// s[i][j] += A[a_row(i)] . B[b_row(j)] over columns [c0, c1); rows ty + 16 i of A, tx + 16 j of B
+template <int DT>
+__device__ __forceinline__ void dots(const float *A, const float *B, int c0, int c1, float (&s)[Tile<DT>::kM][Tile<DT>::kM]) {
+    using C = Tile<DT>;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+#pragma unroll
+    for (int i = 0; i < C::kM; ++i)
+#pragma unroll
+        for (int j = 0; j < C::kM; ++j) s[i][j] = 0.f;
+#pragma unroll 4
+    for (int c = c0; c < c1; c += 4) {
+        float4 x[C::kM], y[C::kM];
+#pragma unroll
+        for (int i = 0; i < C::kM; ++i) x[i] = *(const float4 *)(A + (ty + 16 * i) * C::kLd + c);
+#pragma unroll
+        for (int j = 0; j < C::kM; ++j) y[j] = *(const float4 *)(B + (tx + 16 * j) * C::kLd + c);
+#pragma unroll
+        for (int i = 0; i < C::kM; ++i)
+#pragma unroll
+            for (int j = 0; j < C::kM; ++j) {
+                s[i][j] = fmaf(x[i].x, y[j].x, s[i][j]);
+                s[i][j] = fmaf(x[i].y, y[j].y, s[i][j]);
+                s[i][j] = fmaf(x[i].z, y[j].z, s[i][j]);
+                s[i][j] = fmaf(x[i].w, y[j].w, s[i][j]);
+            }
+    }
+}
+
+// acc[i][ch] += sum_u W[row(i)][u] * B[u][4 tx + 64 ch ..]
+template <int DT>
+__device__ __forceinline__ void weighted_rows(const float *W, const float *B, int ch, float4 (&acc)[Tile<DT>::kM]) {
+    using C = Tile<DT>;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+#pragma unroll 4
+    for (int u = 0; u < C::kRows; u += 4) {
+        float4 w[C::kM];
+#pragma unroll
+        for (int i = 0; i < C::kM; ++i) w[i] = *(const float4 *)(W + (ty + 16 * i) * C::kLp + u);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float4 b = *(const float4 *)(B + (u + e) * C::kLd + 4 * tx + 64 * ch);
+#pragma unroll
+            for (int i = 0; i < C::kM; ++i) {
+                const float x = e == 0 ? w[i].x : e == 1 ? w[i].y : e == 2 ? w[i].z : w[i].w;
+                acc[i].x = fmaf(x, b.x, acc[i].x);
+                acc[i].y = fmaf(x, b.y, acc[i].y);
+                acc[i].z = fmaf(x, b.z, acc[i].z);
+                acc[i].w = fmaf(x, b.w, acc[i].w);
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ float comp(const float4 &v, int e) { return e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w; }
+// column of the caller's tensor behind padded column c, or -1
+template <int DT>
+__device__ __forceinline__ int real_col(int c, int D) {
+    const int hi = c >= DT / 2 ? 1 : 0, cc = c - hi * (DT / 2);
+    return cc < (D >> 1) ? hi * (D >> 1) + cc : -1;
+}
+
+struct SimtArgs {
+    DiffProblem p;
+    DiffPartials part;
+    DiffGrads g;
+    int tiles;                 // query tiles (forward, dQ) or key tiles (dK, dV) per head
+    int gi;                    // query heads per dK / dV item
+    long long prow;            // padded rows of the statistics
+};
+
+template <typename T, int DT>
+__global__ void __launch_bounds__(kThreads)
+diff_simt_kernel(const __grid_constant__ SimtArgs a) {
+    using C = Tile<DT>;
+    extern __shared__ __align__(16) float sm[];
+    float *sQ = sm, *sKV = sQ + C::kRows * C::kLd, *sP1 = sKV + C::kRows * C::kLd, *sP2 = sP1 + C::kRows * C::kLp;
+    const DiffProblem &p = a.p;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    const int tile = a.tiles - 1 - (int)(blockIdx.x % a.tiles);          // later (longer, when causal) tiles first
+    const int bh = (int)(blockIdx.x / a.tiles);
+    const int b = bh / p.H, h = bh - b * p.H, hk = h / (p.H / p.H_kv);
+    const DiffSpan sp = diff_span(p.q_lens, p.kv_lens, b, p.Nq, p.Nk);
+    const int t0 = tile * C::kRows;
+    const T *qb = (const T *)p.q + b * p.sq.b + h * p.sq.h;
+    const T *kb = (const T *)p.k + b * p.sk.b + hk * p.sk.h;
+    const T *vb = (const T *)p.v + b * p.sv.b + hk * p.sv.h;
+    int row_keys[C::kM], keys_end = 0;
+#pragma unroll
+    for (int i = 0; i < C::kM; ++i) row_keys[i] = sp.keys(t0 + ty + 16 * i, p.causal);
+    {
+        const int last = min(t0 + C::kRows, sp.ql) - 1;                  // the last valid row sees the most
+        keys_end = last >= t0 ? sp.keys(last, p.causal) : 0;
+    }
+    const float sl = p.scale * kLog2e;
+    float m[2][C::kM], l[2][C::kM];
+    float4 o[2][C::kCh][C::kM];
+#pragma unroll
+    for (int i = 0; i < C::kM; ++i) {
+        m[0][i] = m[1][i] = -INFINITY;
+        l[0][i] = l[1][i] = 0.f;
+#pragma unroll
+        for (int ch = 0; ch < C::kCh; ++ch) o[0][ch][i] = o[1][ch][i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    if (keys_end > 0) load_tile<T, DT>(sQ, qb, p.sq.n, t0, sp.ql, p.D);
+    for (int u0 = 0; u0 < keys_end; u0 += C::kRows) {
+        __syncthreads();
+        load_tile<T, DT>(sKV, kb, p.sk.n, u0, sp.kl, p.D);
+        __syncthreads();
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            float s[C::kM][C::kM];
+            dots<DT>(sQ, sKV, c * (DT / 2), (c + 1) * (DT / 2), s);
+            float *sP = c ? sP2 : sP1;
+#pragma unroll
+            for (int i = 0; i < C::kM; ++i) {
+                float mx = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < C::kM; ++j) {
+                    s[i][j] = u0 + tx + 16 * j < row_keys[i] ? s[i][j] * sl : -INFINITY;
+                    mx = fmaxf(mx, s[i][j]);
+                }
+#pragma unroll
+                for (int w = 8; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+                const float mn = fmaxf(m[c][i], mx), ref = mn == -INFINITY ? 0.f : mn;
+                const float alpha = exp2f(m[c][i] - ref);                // 2^-inf = 0 at the first visible key
+                float sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < C::kM; ++j) {
+                    const float e = exp2f(s[i][j] - ref);
+                    sum += e;
+                    sP[(ty + 16 * i) * C::kLp + tx + 16 * j] = e;
+                }
+#pragma unroll
+                for (int w = 8; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+                l[c][i] = l[c][i] * alpha + sum;
+                m[c][i] = mn;
+#pragma unroll
+                for (int ch = 0; ch < C::kCh; ++ch) {
+                    o[c][ch][i].x *= alpha; o[c][ch][i].y *= alpha; o[c][ch][i].z *= alpha; o[c][ch][i].w *= alpha;
+                }
+            }
+        }
+        __syncthreads();
+        load_tile<T, DT>(sKV, vb, p.sv.n, u0, sp.kl, p.D);
+        __syncthreads();
+#pragma unroll
+        for (int ch = 0; ch < C::kCh; ++ch) {
+            weighted_rows<DT>(sP1, sKV, ch, o[0][ch]);
+            weighted_rows<DT>(sP2, sKV, ch, o[1][ch]);
+        }
+    }
+    const float lam = __ldg(p.lambda + (p.lambda_count > 1 ? h : 0));
+#pragma unroll
+    for (int i = 0; i < C::kM; ++i) {
+        const int t = t0 + ty + 16 * i;
+        if (t >= p.Nq) continue;
+        const bool any = row_keys[i] > 0;
+        const float i1 = any ? 1.f / l[0][i] : 0.f, i2 = any ? 1.f / l[1][i] : 0.f;
+        T *orow = (T *)p.out + b * p.so.b + h * p.so.h + t * p.so.n;
+        const long long row = (long long)bh * p.Nq + t;
+#pragma unroll
+        for (int ch = 0; ch < C::kCh; ++ch)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int c = real_col<DT>(4 * tx + 64 * ch + e, p.D);
+                if (c < 0) continue;
+                const float o2 = comp(o[1][ch][i], e) * i2;
+                store1(orow + c, comp(o[0][ch][i], e) * i1 - lam * o2);
+                if (p.o2) store1((T *)p.o2 + row * p.D + c, o2);
+            }
+        if (p.lse && tx == 0)
+            p.lse[row] = any ? make_float2(m[0][i] + log2f(l[0][i]), m[1][i] + log2f(l[1][i])) : make_float2(INFINITY, INFINITY);
+    }
+}
+
+// ------------------------------------------------------------------ few query rows: keys split over blocks
+
+constexpr int kSplitKeys = 64, kSplitThreads = 128;
+
+// Rows of a GQA group together: row r of head group hk is query row r % Nq of head hk * g + r / Nq.
+template <typename T, int R>
+__global__ void __launch_bounds__(kSplitThreads)
+diff_simt_split_kernel(const __grid_constant__ SimtArgs a) {
+    extern __shared__ __align__(16) float sm[];
+    const DiffProblem &p = a.p;
+    const int D = p.D, d = D >> 1, ld = D + 1;
+    float *sK = sm;                                    // [64][D + 1], then the V tile
+    float *sQ = sK + kSplitKeys * ld;                  // [D][R]
+    float *sP = sQ + D * R;                            // [64][2][R]
+    float *sRed = sP + kSplitKeys * 2 * R;             // [4 warps][R]
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int g = p.H / p.H_kv, rows = g * p.Nq;
+    const int groups = (rows + R - 1) / R;
+    const int split = (int)(blockIdx.x % a.part.splits);
+    int rest = (int)(blockIdx.x / a.part.splits);
+    const int r0 = (rest % groups) * R; rest /= groups;
+    const int hk = rest % p.H_kv, b = rest / p.H_kv;
+    const DiffSpan sp = diff_span(p.q_lens, p.kv_lens, b, p.Nq, p.Nk);
+    const int per = ((sp.kl + a.part.splits - 1) / a.part.splits + kSplitKeys - 1) / kSplitKeys * kSplitKeys;
+    const int u_lo = min((long long)split * per, (long long)sp.kl), u_hi = min((long long)u_lo + per, (long long)sp.kl);
+    const T *kb = (const T *)p.k + b * p.sk.b + hk * p.sk.h;
+    const T *vb = (const T *)p.v + b * p.sv.b + hk * p.sv.h;
+    int row_keys[R];
+    int keys_end = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        row_keys[r] = r0 + r < rows ? sp.keys((r0 + r) % p.Nq, p.causal) : 0;
+        keys_end = max(keys_end, row_keys[r]);
+    }
+    for (int i = tid; i < D * R; i += kSplitThreads) {
+        const int c = i / R, r = i - c * R;
+        const int h = hk * g + (r0 + r) / p.Nq, t = (r0 + r) % p.Nq;
+        sQ[i] = r0 + r < rows && t < sp.ql
+                    ? load1((const T *)p.q + b * p.sq.b + h * p.sq.h + (long long)t * p.sq.n + c) : 0.f;
+    }
+    const float sl = p.scale * kLog2e;
+    const int cmap = tid >> 6, key = tid & 63;         // scores: one key and one map per thread
+    float m[R], l[R];                                  // of this thread's map
+    float o1[2][R], o2[2][R];                          // features tid, tid + 128
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        m[r] = -INFINITY;
+        l[r] = 0.f;
+        o1[0][r] = o1[1][r] = o2[0][r] = o2[1][r] = 0.f;
+    }
+    __shared__ float sAlpha[2][R];
+    const int end = min(u_hi, keys_end);
+    for (int u0 = u_lo; u0 < end; u0 += kSplitKeys) {
+        __syncthreads();
+        for (int r = warp; r < kSplitKeys; r += kSplitThreads / 32)
+            for (int c = lane; c < D; c += 32) sK[r * ld + c] = u0 + r < end ? load1(kb + (long long)(u0 + r) * p.sk.n + c) : 0.f;
+        __syncthreads();
+        float s[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) s[r] = 0.f;
+        const float *krow = sK + key * ld + cmap * d, *qcol = sQ + cmap * d * R;
+        for (int c = 0; c < d; ++c) {
+            const float x = krow[c];
+#pragma unroll
+            for (int r = 0; r < R; ++r) s[r] = fmaf(x, qcol[c * R + r], s[r]);
+        }
+        float mx[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            s[r] = u0 + key < min(end, row_keys[r]) ? s[r] * sl : -INFINITY;
+            mx[r] = s[r];
+#pragma unroll
+            for (int w = 16; w > 0; w >>= 1) mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], w));
+        }
+        if (lane == 0)
+#pragma unroll
+            for (int r = 0; r < R; ++r) sRed[warp * R + r] = mx[r];
+        __syncthreads();                               // (all of K has been read, too)
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const float both = fmaxf(sRed[(warp & ~1) * R + r], sRed[(warp | 1) * R + r]);
+            const float mn = fmaxf(m[r], both), ref = mn == -INFINITY ? 0.f : mn;
+            const float alpha = exp2f(m[r] - ref);
+            const float e = exp2f(s[r] - ref);
+            sP[(key * 2 + cmap) * R + r] = e;
+            l[r] = l[r] * alpha + e;                   // this thread's keys; summed over the threads at the end
+            m[r] = mn;
+            if (key == 0) sAlpha[cmap][r] = alpha;
+        }
+        for (int r = warp; r < kSplitKeys; r += kSplitThreads / 32)
+            for (int c = lane; c < D; c += 32) sK[r * ld + c] = u0 + r < end ? load1(vb + (long long)(u0 + r) * p.sv.n + c) : 0.f;
+        __syncthreads();
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+            const int c = tid + f * kSplitThreads;
+            if (c >= D) break;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                o1[f][r] *= sAlpha[0][r];
+                o2[f][r] *= sAlpha[1][r];
+            }
+#pragma unroll 4
+            for (int u = 0; u < kSplitKeys; ++u) {
+                const float x = sK[u * ld + c];
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    o1[f][r] = fmaf(sP[(u * 2) * R + r], x, o1[f][r]);
+                    o2[f][r] = fmaf(sP[(u * 2 + 1) * R + r], x, o2[f][r]);
+                }
+            }
+        }
+    }
+    // sums of l over the 64 threads of each map
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int w = 16; w > 0; w >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], w);
+    __syncthreads();
+    if (lane == 0)
+#pragma unroll
+        for (int r = 0; r < R; ++r) sRed[warp * R + r] = l[r];
+    if (key == 0)
+#pragma unroll
+        for (int r = 0; r < R; ++r) sAlpha[cmap][r] = m[r];
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (r0 + r >= rows) break;
+        const int h = hk * g + (r0 + r) / p.Nq, t = (r0 + r) % p.Nq;
+        const long long row = ((long long)b * p.H + h) * p.Nq + t;
+        const long long slot = row * a.part.splits + split;
+        if (tid == 0)
+            a.part.ml[slot] = make_float4(sAlpha[0][r], sRed[r] + sRed[R + r], sAlpha[1][r], sRed[2 * R + r] + sRed[3 * R + r]);
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+            const int c = tid + f * kSplitThreads;
+            if (c >= D) break;
+            a.part.acc[slot * 2 * D + c] = o1[f][r];
+            a.part.acc[slot * 2 * D + D + c] = o2[f][r];
+        }
+    }
+}
+
+// One warp per query row: joins the key ranges.  Ranges that saw nothing have m = -inf, l = 0 and sums of 0.
+template <typename T>
+__global__ void __launch_bounds__(128)
+diff_combine_kernel(const __grid_constant__ SimtArgs a) {
+    const DiffProblem &p = a.p;
+    griddep_wait();
+    const long long row = blockIdx.x * 4ll + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    if (row >= (long long)p.B * p.H * p.Nq) return;
+    const int t = (int)(row % p.Nq);
+    const int bh = (int)(row / p.Nq), b = bh / p.H, h = bh - b * p.H;
+    const int ns = a.part.splits, D = p.D;
+    const float4 *ml = a.part.ml + row * ns;
+    float m1 = -INFINITY, m2 = -INFINITY;
+    for (int s = lane; s < ns; s += 32) {
+        const float4 x = ml[s];
+        m1 = fmaxf(m1, x.x);
+        m2 = fmaxf(m2, x.z);
+    }
+#pragma unroll
+    for (int w = 16; w > 0; w >>= 1) {
+        m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, w));
+        m2 = fmaxf(m2, __shfl_xor_sync(0xffffffffu, m2, w));
+    }
+    const bool any = m1 != -INFINITY;
+    float l1 = 0.f, l2 = 0.f;
+    float acc1[8], acc2[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc1[i] = acc2[i] = 0.f;
+    if (any) {
+#pragma unroll 4
+        for (int s = 0; s < ns; ++s) {
+            const float4 x = ml[s];
+            const float w1 = exp2f(x.x - m1), w2 = exp2f(x.z - m2);
+            l1 = fmaf(x.y, w1, l1);
+            l2 = fmaf(x.w, w2, l2);
+            const float *o = a.part.acc + (row * ns + s) * 2 * D;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int c = lane + 32 * i;
+                if (c >= D) break;
+                acc1[i] = fmaf(o[c], w1, acc1[i]);
+                acc2[i] = fmaf(o[D + c], w2, acc2[i]);
+            }
+        }
+    }
+    const float lam = __ldg(p.lambda + (p.lambda_count > 1 ? h : 0));
+    const float i1 = any ? 1.f / l1 : 0.f, i2 = any ? 1.f / l2 : 0.f;
+    T *orow = (T *)p.out + b * p.so.b + h * p.so.h + (long long)t * p.so.n;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int c = lane + 32 * i;
+        if (c >= D) break;
+        const float o2 = acc2[i] * i2;
+        store1(orow + c, acc1[i] * i1 - lam * o2);
+        if (p.o2) store1((T *)p.o2 + row * D + c, o2);
+    }
+    if (p.lse && lane == 0)
+        p.lse[row] = any ? make_float2(m1 + log2f(l1), m2 + log2f(l2)) : make_float2(INFINITY, INFINITY);
+}
+
+// ------------------------------------------------------------------ backward
+
+// One warp per row: d_2 = <dout, A_2 V>, d_1 = <dout, A_1 V> = <dout, out> + lambda d_2.
+template <typename T>
+__global__ void __launch_bounds__(128)
+diff_stats_kernel(const __grid_constant__ SimtArgs a, float4 *stats) {
+    const DiffProblem &p = a.p;
+    const long long idx = blockIdx.x * 4ll + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    const int bh = (int)(idx / a.prow), t = (int)(idx - bh * a.prow);
+    if (bh >= p.B * p.H) return;
+    const int b = bh / p.H, h = bh - b * p.H;
+    float2 lse = make_float2(INFINITY, INFINITY);
+    float d1 = 0.f, d2 = 0.f;
+    if (t < p.Nq) lse = p.lse[(long long)bh * p.Nq + t];
+    if (lse.x < INFINITY) {
+        const T *g = (const T *)p.dout + b * p.sdo.b + h * p.sdo.h + (long long)t * p.sdo.n;
+        const T *o = (const T *)p.out + b * p.so.b + h * p.so.h + (long long)t * p.so.n;
+        const T *o2 = (const T *)p.o2 + ((long long)bh * p.Nq + t) * p.D;
+        for (int c = lane; c < p.D; c += 32) {
+            const float x = load1(g + c);
+            d1 = fmaf(x, load1(o + c), d1);
+            d2 = fmaf(x, load1(o2 + c), d2);
+        }
+#pragma unroll
+        for (int w = 16; w > 0; w >>= 1) {
+            d1 += __shfl_xor_sync(0xffffffffu, d1, w);
+            d2 += __shfl_xor_sync(0xffffffffu, d2, w);
+        }
+        d1 = fmaf(__ldg(p.lambda + (p.lambda_count > 1 ? h : 0)), d2, d1);
+    }
+    if (lane == 0) stats[idx] = make_float4(lse.x, lse.y, d1, d2);
+}
+
+// dQ of one query tile and its share of dlambda: walks the key tiles the rows see
+template <typename T, int DT>
+__global__ void __launch_bounds__(kThreads)
+diff_simt_dq_kernel(const __grid_constant__ SimtArgs a) {
+    using C = Tile<DT>;
+    extern __shared__ __align__(16) float sm[];
+    float *sQ = sm, *sG = sQ + C::kRows * C::kLd, *sK = sG + C::kRows * C::kLd, *sV = sK + C::kRows * C::kLd;
+    float *sS1 = sV + C::kRows * C::kLd, *sS2 = sS1 + C::kRows * C::kLp;
+    __shared__ float s_red[kThreads / 32];
+    const DiffProblem &p = a.p;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    const int tile = a.tiles - 1 - (int)(blockIdx.x % a.tiles);
+    const int bh = (int)(blockIdx.x / a.tiles);
+    const int b = bh / p.H, h = bh - b * p.H, hk = h / (p.H / p.H_kv);
+    const DiffSpan sp = diff_span(p.q_lens, p.kv_lens, b, p.Nq, p.Nk);
+    const int t0 = tile * C::kRows;
+    const T *kb = (const T *)p.k + b * p.sk.b + hk * p.sk.h;
+    const T *vb = (const T *)p.v + b * p.sv.b + hk * p.sv.h;
+    const int last = min(t0 + C::kRows, sp.ql) - 1;
+    const int keys_end = last >= t0 ? sp.keys(last, p.causal) : 0;
+    int row_keys[C::kM];
+    float4 st[C::kM];
+#pragma unroll
+    for (int i = 0; i < C::kM; ++i) {
+        const int t = t0 + ty + 16 * i;
+        row_keys[i] = sp.keys(t, p.causal);
+        st[i] = t < p.Nq ? __ldg(a.g.stats + bh * a.prow + t) : make_float4(INFINITY, INFINITY, 0.f, 0.f);
+    }
+    const float sl = p.scale * kLog2e, lam = __ldg(p.lambda + (p.lambda_count > 1 ? h : 0));
+    float4 dq[C::kCh][C::kM];
+#pragma unroll
+    for (int ch = 0; ch < C::kCh; ++ch)
+#pragma unroll
+        for (int i = 0; i < C::kM; ++i) dq[ch][i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    float dlam = 0.f;
+    if (keys_end > 0) {
+        load_tile<T, DT>(sQ, (const T *)p.q + b * p.sq.b + h * p.sq.h, p.sq.n, t0, sp.ql, p.D);
+        load_tile<T, DT>(sG, (const T *)p.dout + b * p.sdo.b + h * p.sdo.h, p.sdo.n, t0, sp.ql, p.D);
+    }
+    for (int u0 = 0; u0 < keys_end; u0 += C::kRows) {
+        __syncthreads();
+        load_tile<T, DT>(sK, kb, p.sk.n, u0, sp.kl, p.D);
+        load_tile<T, DT>(sV, vb, p.sv.n, u0, sp.kl, p.D);
+        __syncthreads();
+        float s[C::kM][C::kM], dp[C::kM][C::kM];
+        dots<DT>(sG, sV, 0, DT, dp);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            dots<DT>(sQ, sK, c * (DT / 2), (c + 1) * (DT / 2), s);
+            float *sS = c ? sS2 : sS1;
+#pragma unroll
+            for (int i = 0; i < C::kM; ++i)
+#pragma unroll
+                for (int j = 0; j < C::kM; ++j) {
+                    const bool vis = u0 + tx + 16 * j < row_keys[i];
+                    const float w = vis ? exp2f(fmaf(s[i][j], sl, -(c ? st[i].y : st[i].x))) : 0.f;
+                    if (c) dlam = fmaf(w, dp[i][j], dlam);
+                    const float f = c ? -lam * p.scale : p.scale;
+                    sS[(ty + 16 * i) * C::kLp + tx + 16 * j] = w * (dp[i][j] - (c ? st[i].w : st[i].z)) * f;
+                }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int ch = 0; ch < C::kCh; ++ch) weighted_rows<DT>(4 * tx + 64 * ch < DT / 2 ? sS1 : sS2, sK, ch, dq[ch]);
+    }
+#pragma unroll
+    for (int i = 0; i < C::kM; ++i) {
+        const int t = t0 + ty + 16 * i;
+        if (t >= p.Nq) continue;
+        T *row = (T *)a.g.dq + ((long long)bh * p.Nq + t) * p.D;
+#pragma unroll
+        for (int ch = 0; ch < C::kCh; ++ch)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int c = real_col<DT>(4 * tx + 64 * ch + e, p.D);
+                if (c >= 0) store1(row + c, comp(dq[ch][i], e));
+            }
+    }
+#pragma unroll
+    for (int w = 16; w > 0; w >>= 1) dlam += __shfl_xor_sync(0xffffffffu, dlam, w);
+    if ((threadIdx.x & 31) == 0) s_red[threadIdx.x >> 5] = dlam;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        float x = 0.f;
+        for (int i = 0; i < kThreads / 32; ++i) x += s_red[i];
+        a.g.dlam_part[(long long)bh * a.tiles + tile] = x;
+    }
+}
+
+// dK, dV of one key tile: walks the query heads of its item and, per head, the query tiles that see it
+template <typename T, int DT>
+__global__ void __launch_bounds__(kThreads)
+diff_simt_dkv_kernel(const __grid_constant__ SimtArgs a) {
+    using C = Tile<DT>;
+    extern __shared__ __align__(16) float sm[];
+    float *sK = sm, *sV = sK + C::kRows * C::kLd, *sQ = sV + C::kRows * C::kLd, *sG = sQ + C::kRows * C::kLd;
+    float *sA = sG + C::kRows * C::kLd, *sS1 = sA + C::kRows * C::kLp, *sS2 = sS1 + C::kRows * C::kLp;
+    __shared__ float4 s_st[C::kRows];
+    const DiffProblem &p = a.p;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    const int tile = (int)(blockIdx.x % a.tiles);                        // earlier (longer, when causal) tiles first
+    int rest = (int)(blockIdx.x / a.tiles);
+    const int hs = rest % a.g.hsplit; rest /= a.g.hsplit;
+    const int hk = rest % p.H_kv, b = rest / p.H_kv;
+    const int g = p.H / p.H_kv;
+    const DiffSpan sp = diff_span(p.q_lens, p.kv_lens, b, p.Nq, p.Nk);
+    const int u0 = tile * C::kRows;
+    const float sl = p.scale * kLog2e;
+    float4 dk[C::kCh][C::kM], dv[C::kCh][C::kM];
+#pragma unroll
+    for (int ch = 0; ch < C::kCh; ++ch)
+#pragma unroll
+        for (int i = 0; i < C::kM; ++i) dk[ch][i] = dv[ch][i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    // first row that sees the tile's first key
+    const int t_lo = p.causal ? max(0, u0 - sp.off) / C::kRows * C::kRows : 0;
+    if (u0 < sp.kl && t_lo < sp.ql) {
+        load_tile<T, DT>(sK, (const T *)p.k + b * p.sk.b + hk * p.sk.h, p.sk.n, u0, sp.kl, p.D);
+        load_tile<T, DT>(sV, (const T *)p.v + b * p.sv.b + hk * p.sv.h, p.sv.n, u0, sp.kl, p.D);
+        for (int hh = 0; hh < a.gi; ++hh) {
+            const int h = hk * g + hs * a.gi + hh;
+            const int bh = b * p.H + h;
+            const float lam = __ldg(p.lambda + (p.lambda_count > 1 ? h : 0));
+            for (int t0 = t_lo; t0 < sp.ql; t0 += C::kRows) {
+                __syncthreads();
+                load_tile<T, DT>(sQ, (const T *)p.q + b * p.sq.b + h * p.sq.h, p.sq.n, t0, sp.ql, p.D);
+                load_tile<T, DT>(sG, (const T *)p.dout + b * p.sdo.b + h * p.sdo.h, p.sdo.n, t0, sp.ql, p.D);
+                if (threadIdx.x < C::kRows)
+                    s_st[threadIdx.x] = t0 + (int)threadIdx.x < p.Nq ? __ldg(a.g.stats + bh * a.prow + t0 + threadIdx.x)
+                                                                    : make_float4(INFINITY, INFINITY, 0.f, 0.f);
+                __syncthreads();
+                float s[C::kM][C::kM], dp[C::kM][C::kM], w1[C::kM][C::kM];
+                dots<DT>(sV, sG, 0, DT, dp);                             // rows: keys, columns: query rows
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    dots<DT>(sK, sQ, c * (DT / 2), (c + 1) * (DT / 2), s);
+                    float *sS = c ? sS2 : sS1;
+#pragma unroll
+                    for (int j = 0; j < C::kM; ++j) {
+                        const float4 st = s_st[tx + 16 * j];
+                        const int keys = sp.keys(t0 + tx + 16 * j, p.causal);
+#pragma unroll
+                        for (int i = 0; i < C::kM; ++i) {
+                            const bool vis = u0 + ty + 16 * i < keys;
+                            const float w = vis ? exp2f(fmaf(s[i][j], sl, -(c ? st.y : st.x))) : 0.f;
+                            const float f = c ? -lam * p.scale : p.scale;
+                            const int at = (ty + 16 * i) * C::kLp + tx + 16 * j;
+                            sS[at] = w * (dp[i][j] - (c ? st.w : st.z)) * f;
+                            if (c) sA[at] = w1[i][j] - lam * w;
+                            else w1[i][j] = w;
+                        }
+                    }
+                }
+                __syncthreads();
+#pragma unroll
+                for (int ch = 0; ch < C::kCh; ++ch) {
+                    weighted_rows<DT>(sA, sG, ch, dv[ch]);
+                    weighted_rows<DT>(4 * tx + 64 * ch < DT / 2 ? sS1 : sS2, sQ, ch, dk[ch]);
+                }
+            }
+        }
+    }
+    const long long kv_elems = (long long)p.B * p.H_kv * p.Nk * p.D;
+#pragma unroll
+    for (int i = 0; i < C::kM; ++i) {
+        const int u = u0 + ty + 16 * i;
+        if (u >= p.Nk) continue;
+        const long long row = (((long long)b * p.H_kv + hk) * p.Nk + u) * p.D;
+#pragma unroll
+        for (int ch = 0; ch < C::kCh; ++ch)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int c = real_col<DT>(4 * tx + 64 * ch + e, p.D);
+                if (c < 0) continue;
+                if (a.g.hsplit > 1) {
+                    a.g.part[hs * kv_elems + row + c] = comp(dk[ch][i], e);
+                    a.g.part[(a.g.hsplit + hs) * kv_elems + row + c] = comp(dv[ch][i], e);
+                } else {
+                    store1((T *)a.g.dk + row + c, comp(dk[ch][i], e));
+                    store1((T *)a.g.dv + row + c, comp(dv[ch][i], e));
+                }
+            }
+    }
+}
+
+// dK, dV = sums of the partials of a group's head chunks, in their order
+template <typename T>
+__global__ void __launch_bounds__(256)
+diff_group_sum_kernel(const float *part, int hsplit, long long n, T *dk, T *dv) {
+    for (long long i = (blockIdx.x * 256ll + threadIdx.x) * 2; i < 2 * n; i += gridDim.x * 512ll) {
+        const long long j = i < n ? i : i - n;                 // (n is even: D is)
+        const float *src = part + (i < n ? 0 : hsplit * n) + j;
+        float2 s = make_float2(0.f, 0.f);
+        for (int h = 0; h < hsplit; ++h) {
+            const float2 x = *(const float2 *)(src + h * n);
+            s.x += x.x;
+            s.y += x.y;
+        }
+        T *dst = (i < n ? dk : dv) + j;
+        store1(dst, s.x);
+        store1(dst + 1, s.y);
+    }
+}
+
+// dlambda[i] = -sum of the tiles' sums of A_2 o dA, over batch entries (and heads, when there is one lambda); one block per
+// lambda, every thread its terms in order, then a fixed tree
+__global__ void __launch_bounds__(256)
+diff_dlambda_kernel(const float *part, int B, int H, int tiles, int lambda_count, float *dlambda) {
+    __shared__ double s[256];
+    double x = 0.;
+    const int heads = lambda_count > 1 ? 1 : H;
+    const long long n = (long long)B * heads * tiles;
+    for (long long i = threadIdx.x; i < n; i += 256) {
+        const long long bh = i / tiles, t = i - bh * tiles;
+        const long long b = bh / heads, h = lambda_count > 1 ? blockIdx.x : bh - b * heads;
+        x += part[(b * H + h) * tiles + t];
+    }
+    s[threadIdx.x] = x;
+    for (int w = 128; w > 0; w >>= 1) {
+        __syncthreads();
+        if (threadIdx.x < w) s[threadIdx.x] += s[threadIdx.x + w];
+    }
+    if (threadIdx.x == 0) dlambda[blockIdx.x] = (float)-s[0];
+}
+
+template <typename K>
+int allow_smem(K kern, size_t bytes, PerDeviceOnce &once) {
+    int dev = 0;
+    current_device_sms(&dev);
+    if (once.is_done(dev)) return TA_OK;
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e != cudaSuccess) return cuda_fail(e);
+    once.mark(dev);
+    return TA_OK;
+}
+
+template <typename T, int DT>
+int launch_tile(const DiffProblem &p) {
+    using C = Tile<DT>;
+    constexpr size_t smem = (2 * C::kRows * C::kLd + 2 * C::kRows * C::kLp) * sizeof(float);
+    static PerDeviceOnce once;
+    int rc = allow_smem(diff_simt_kernel<T, DT>, smem, once);
+    if (rc != TA_OK) return rc;
+    SimtArgs a = {};
+    a.p = p;
+    a.tiles = (p.Nq + C::kRows - 1) / C::kRows;
+    const long long blocks = (long long)p.B * p.H * a.tiles;
+    if (blocks > 0x7FFFFFFFll) return TA_ERR_TOO_LARGE;
+    return launch_kernel(diff_simt_kernel<T, DT>, (unsigned)blocks, kThreads, smem, p.stream, false, a);
+}
+
+template <typename T, int R>
+int launch_split(const DiffProblem &p, const DiffPartials &part) {
+    const size_t smem = (kSplitKeys * (p.D + 1) + p.D * R + kSplitKeys * 2 * R + 4 * R) * sizeof(float);
+    static PerDeviceOnce once;
+    int rc = allow_smem(diff_simt_split_kernel<T, R>, (kSplitKeys * 257 + 256 * R + kSplitKeys * 2 * R + 4 * R) * sizeof(float), once);
+    if (rc != TA_OK) return rc;
+    SimtArgs a = {};
+    a.p = p;
+    a.part = part;
+    const int rows = p.H / p.H_kv * p.Nq;
+    const long long blocks = (long long)p.B * p.H_kv * ((rows + R - 1) / R) * part.splits;
+    if (blocks > 0x7FFFFFFFll) return TA_ERR_TOO_LARGE;
+    return launch_kernel(diff_simt_split_kernel<T, R>, (unsigned)blocks, kSplitThreads, smem, p.stream, false, a);
+}
+
+template <typename T>
+int launch_split_rows(const DiffProblem &p, const DiffPartials &part) {
+    const int rows = p.H / p.H_kv * p.Nq;
+    if (rows == 1) return launch_split<T, 1>(p, part);
+    if (rows == 2) return launch_split<T, 2>(p, part);
+    if (rows <= 4) return launch_split<T, 4>(p, part);
+    return launch_split<T, 8>(p, part);
+}
+
+template <typename T, int DT>
+int launch_bwd(const DiffProblem &p, const DiffGrads &g) {
+    using C = Tile<DT>;
+    constexpr size_t smem_q = (4 * C::kRows * C::kLd + 2 * C::kRows * C::kLp) * sizeof(float);
+    constexpr size_t smem_k = (4 * C::kRows * C::kLd + 3 * C::kRows * C::kLp) * sizeof(float);
+    static PerDeviceOnce once_q, once_k;
+    int rc = allow_smem(diff_simt_dq_kernel<T, DT>, smem_q, once_q);
+    if (rc == TA_OK) rc = allow_smem(diff_simt_dkv_kernel<T, DT>, smem_k, once_k);
+    if (rc != TA_OK) return rc;
+    SimtArgs a = {};
+    a.p = p;
+    a.g = g;
+    a.prow = diff_padded_rows(p.Nq);
+    a.gi = p.H / p.H_kv / g.hsplit;
+    a.tiles = (p.Nq + C::kRows - 1) / C::kRows;
+    const long long qblocks = (long long)p.B * p.H * a.tiles;
+    const int ktiles = (p.Nk + C::kRows - 1) / C::kRows;
+    const long long kblocks = (long long)p.B * p.H_kv * g.hsplit * ktiles;
+    if (qblocks > 0x7FFFFFFFll || kblocks > 0x7FFFFFFFll) return TA_ERR_TOO_LARGE;
+    rc = launch_kernel(diff_simt_dq_kernel<T, DT>, (unsigned)qblocks, kThreads, smem_q, p.stream, false, a);
+    if (rc != TA_OK) return rc;
+    a.tiles = ktiles;
+    return launch_kernel(diff_simt_dkv_kernel<T, DT>, (unsigned)kblocks, kThreads, smem_k, p.stream, false, a);
+}
+
+}  // namespace
+
+int diff_simt_tile(int D) { return D > 128 ? 32 : 64; }
+
+int launch_diff_simt(const DiffProblem &p) {
+    if (p.dtype == TA_DTYPE_F32)
+        return p.D <= 64 ? launch_tile<float, 64>(p) : p.D <= 128 ? launch_tile<float, 128>(p) : launch_tile<float, 256>(p);
+    return p.D <= 64 ? launch_tile<__nv_bfloat16, 64>(p)
+                     : p.D <= 128 ? launch_tile<__nv_bfloat16, 128>(p) : launch_tile<__nv_bfloat16, 256>(p);
+}
+
+int launch_diff_simt_split(const DiffProblem &p, const DiffPartials &part) {
+    return p.dtype == TA_DTYPE_F32 ? launch_split_rows<float>(p, part) : launch_split_rows<__nv_bfloat16>(p, part);
+}
+
+int launch_diff_combine(const DiffProblem &p, const DiffPartials &part) {
+    SimtArgs a = {};
+    a.p = p;
+    a.part = part;
+    const long long blocks = ((long long)p.B * p.H * p.Nq + 3) / 4;
+    if (blocks > 0x7FFFFFFFll) return TA_ERR_TOO_LARGE;
+    if (p.dtype == TA_DTYPE_F32)
+        return launch_kernel(diff_combine_kernel<float>, (unsigned)blocks, 128, 0, p.stream, true, a);
+    return launch_kernel(diff_combine_kernel<__nv_bfloat16>, (unsigned)blocks, 128, 0, p.stream, true, a);
+}
+
+int launch_diff_stats(const DiffProblem &p, float4 *stats) {
+    SimtArgs a = {};
+    a.p = p;
+    a.prow = diff_padded_rows(p.Nq);
+    const long long blocks = ((long long)p.B * p.H * a.prow + 3) / 4;
+    if (blocks > 0x7FFFFFFFll) return TA_ERR_TOO_LARGE;
+    if (p.dtype == TA_DTYPE_F32)
+        return launch_kernel(diff_stats_kernel<float>, (unsigned)blocks, 128, 0, p.stream, false, a, stats);
+    return launch_kernel(diff_stats_kernel<__nv_bfloat16>, (unsigned)blocks, 128, 0, p.stream, false, a, stats);
+}
+
+int launch_diff_simt_bwd(const DiffProblem &p, const DiffGrads &g) {
+    if (p.dtype == TA_DTYPE_F32)
+        return p.D <= 64 ? launch_bwd<float, 64>(p, g) : p.D <= 128 ? launch_bwd<float, 128>(p, g) : launch_bwd<float, 256>(p, g);
+    return p.D <= 64 ? launch_bwd<__nv_bfloat16, 64>(p, g)
+                     : p.D <= 128 ? launch_bwd<__nv_bfloat16, 128>(p, g) : launch_bwd<__nv_bfloat16, 256>(p, g);
+}
+
+int launch_diff_group_sum(const DiffProblem &p, const DiffGrads &g) {
+    const long long n = (long long)p.B * p.H_kv * p.Nk * p.D;
+    long long blocks = (n + 255) / 256;
+    if (blocks > 148 * 16) blocks = 148 * 16;
+    if (p.dtype == TA_DTYPE_F32)
+        return launch_kernel(diff_group_sum_kernel<float>, (unsigned)blocks, 256, 0, p.stream, false, (const float *)g.part,
+                             g.hsplit, n, (float *)g.dk, (float *)g.dv);
+    return launch_kernel(diff_group_sum_kernel<__nv_bfloat16>, (unsigned)blocks, 256, 0, p.stream, false, (const float *)g.part,
+                         g.hsplit, n, (__nv_bfloat16 *)g.dk, (__nv_bfloat16 *)g.dv);
+}
+
+int launch_diff_dlambda(const DiffProblem &p, const DiffGrads &g, int tiles, float *dlambda) {
+    return launch_kernel(diff_dlambda_kernel, (unsigned)p.lambda_count, 256, 0, p.stream, false, (const float *)g.dlam_part,
+                         p.B, p.H, tiles, p.lambda_count, dlambda);
+}
+
+}  // namespace ta

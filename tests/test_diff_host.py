@@ -1,0 +1,129 @@
+"""Differential attention without a GPU: refusals come before any CUDA call, workspace sizes, and pins of the reference
+that the GPU tests compare with."""
+import ctypes
+
+import numpy as np
+import pytest
+
+import diff_reference as ref
+import paper_2410_20926_b200 as ta
+from paper_2410_20926_b200 import api
+
+M = 1 << 24
+
+
+def fwd(q=M, k=2 * M, v=3 * M, out=4 * M, lam=5 * M, lambda_count=None, B=1, H=4, H_kv=2, Nq=8, Nk=8, D=64, causal=True, **kw):
+    return ta.ta_diff_forward(q, k, v, out, lam, H if lambda_count is None else lambda_count, B, H, H_kv, Nq, Nk, D,
+                              causal, stream=0, check=False, **kw)
+
+
+COMMON = [
+    (dict(q=0), "INVALID_ARG"), (dict(k=0), "INVALID_ARG"), (dict(v=0), "INVALID_ARG"), (dict(out=0), "INVALID_ARG"),
+    (dict(lam=0), "INVALID_ARG"), (dict(lambda_count=3), "INVALID_ARG"), (dict(lambda_count=0), "INVALID_ARG"),
+    (dict(B=0), "INVALID_ARG"), (dict(Nq=0), "INVALID_ARG"), (dict(Nk=0), "INVALID_ARG"), (dict(H_kv=0), "INVALID_ARG"),
+    (dict(H=3), "SHAPE"), (dict(D=63), "UNSUPPORTED"), (dict(D=258), "UNSUPPORTED"), (dict(D=0), "INVALID_ARG"),
+    (dict(dtype=2), "UNSUPPORTED"), (dict(flags=2), "UNSUPPORTED"), (dict(softmax_scale=float("nan")), "INVALID_ARG"),
+    (dict(softmax_scale=float("inf")), "INVALID_ARG"), (dict(q=M + 1), "ALIGNMENT"), (dict(lam=5 * M + 2), "ALIGNMENT"),
+    (dict(workspace=M // 2 + 16, workspace_bytes=1 << 30), "ALIGNMENT"), (dict(B=1 << 20, H=1 << 12), "TOO_LARGE"),
+]
+
+
+@pytest.mark.parametrize("kw,status", COMMON + [
+    (dict(out=M), "INVALID_ARG"), (dict(out=M + 64), "INVALID_ARG"), (dict(out=3 * M), "INVALID_ARG"),
+    (dict(out_strides=(0, 0, 64)), "INVALID_ARG"), (dict(saved=8 * M + 16), "ALIGNMENT"),
+    (dict(workspace=M // 2, workspace_bytes=16), "WORKSPACE"),
+])
+def test_forward_refusals(kw, status):
+    assert fwd(**kw) == getattr(ta, "TA_ERR_" + status)
+
+
+def bwd(dout=6 * M, q=M, k=2 * M, v=3 * M, out=4 * M, lam=5 * M, lambda_count=None, saved=7 * M, dq=8 * M, dk=9 * M,
+        dv=10 * M, dlambda=11 * M, B=1, H=4, H_kv=2, Nq=8, Nk=8, D=64, causal=True, **kw):
+    return ta.ta_diff_backward(dout, q, k, v, out, lam, H if lambda_count is None else lambda_count, saved, dq, dk, dv,
+                               dlambda, B, H, H_kv, Nq, Nk, D, causal, stream=0, check=False, **kw)
+
+
+@pytest.mark.parametrize("kw,status", COMMON + [
+    (dict(dout=0), "INVALID_ARG"), (dict(saved=0), "INVALID_ARG"), (dict(dq=0), "INVALID_ARG"), (dict(dk=0), "INVALID_ARG"),
+    (dict(dv=0), "INVALID_ARG"), (dict(dlambda=0), "INVALID_ARG"), (dict(dq=M), "INVALID_ARG"), (dict(dk=9 * M + 8), "ALIGNMENT"),
+    (dict(dv=9 * M), "INVALID_ARG"), (dict(dv=9 * M + 64), "INVALID_ARG"), (dict(saved=7 * M + 8), "ALIGNMENT"),
+    (dict(dlambda=11 * M + 2), "ALIGNMENT"), (dict(workspace=M // 2, workspace_bytes=16), "WORKSPACE"),
+])
+def test_backward_refusals(kw, status):
+    assert bwd(**kw) == getattr(ta, "TA_ERR_" + status)
+
+
+def test_struct_sizes_are_checked():
+    lib = api.load()
+    for cls, fn in ((api.ta_diff_params, lib.ta_diff_forward), (api.ta_diff_bwd_params, lib.ta_diff_backward)):
+        p = cls()
+        p.struct_bytes = 8
+        assert fn(ctypes.byref(p)) == ta.TA_ERR_INVALID_ARG
+        assert fn(None) == ta.TA_ERR_INVALID_ARG
+
+
+def test_workspace_bytes():
+    up = lambda x: (x + 255) // 256 * 256  # noqa: E731
+    size = ta.ta_diff_workspace_bytes
+    assert size(2, 4, 2, 100, 100, 64, ta.TA_DTYPE_BF16, ta.TA_DIFF_WS_SAVED) == up(800 * 8) + up(800 * 64 * 2)
+    assert size(2, 4, 2, 100, 100, 64, ta.TA_DTYPE_F32, ta.TA_DIFF_WS_SAVED) == up(800 * 8) + up(800 * 64 * 4)
+    assert size(2, 4, 2, 1, 100, 64) > 0                       # few rows: partial sums
+    assert size(2, 4, 2, 100, 100, 64, mode=ta.TA_DIFF_WS_BACKWARD) >= 8 * 128 * 16
+    assert size(2, 4, 3, 100, 100, 64) == 0 and size(2, 4, 2, 100, 100, 64, mode=9) == 0
+
+
+def test_torch_binding_refuses():
+    import torch
+    q = torch.zeros(1, 2, 4, 16)
+    with pytest.raises(ValueError, match="CUDA"):
+        ta.differential_attention(q, q, q, torch.zeros(2))
+
+
+# ------------------------------------------------------------------ the reference
+
+def data(seed=0, B=1, H=2, Hk=1, Nq=5, Nk=7, D=6):
+    rng = np.random.default_rng(seed)
+    return (rng.standard_normal((B, H, Nq, D)), rng.standard_normal((B, Hk, Nk, D)), rng.standard_normal((B, Hk, Nk, D)),
+            rng.uniform(0.1, 0.9, H), rng.standard_normal((B, H, Nq, D)))
+
+
+def test_reference_is_textbook_attention_at_lambda_zero_and_cancels_equal_maps():
+    from scipy.special import softmax
+    q, k, v, _, _ = data()
+    out = ref.run(q, k, v, 0.0, False)["out"][0]
+    want = softmax(q[0, 1, :, :3] @ k[0, 0, :, :3].T / np.sqrt(3), -1) @ v[0, 0]
+    assert np.abs(out[0, 1] - want).max() < 1e-14
+    q[..., 3:], k[..., 3:] = q[..., :3], k[..., :3]
+    assert np.abs(ref.run(q, k, v, 1.0, True)["out"][0]).max() < 1e-14
+
+
+def test_reference_positions_and_lengths():
+    q, k, v, lam, _ = data(Nq=7, Nk=7)
+    full = ref.run(q, k, v, lam, True)["out"][0]
+    for t in range(7):                                   # one token against a cache filled up to it
+        one = ref.run(q[:, :, t:t + 1], k, v, lam, True, kv_lens=[t + 1])["out"][0]
+        assert np.abs(one[0, :, 0] - full[0, :, t]).max() < 1e-14
+    part = ref.run(q, k, v, lam, True, q_lens=[4], kv_lens=[4])["out"][0]
+    assert np.abs(part[0, :, :4] - full[0, :, :4]).max() < 1e-14 and not part[0, :, 4:].any()
+    empty = ref.run(q, k, v, lam, True, q_lens=[5], kv_lens=[2])["out"][0]
+    assert not empty[0, :, :3].any() and empty[0, :, 3:5].any()
+    assert not ref.run(q, k, v, lam, False, kv_lens=[0])["out"][0].any()
+
+
+@pytest.mark.parametrize("causal,ql,kl", [(False, None, None), (True, None, None), (True, [4], [3])])
+def test_reference_gradients_against_differences(causal, ql, kl):
+    q, k, v, lam, do = data(3)
+    got = ref.run(q, k, v, lam, causal, q_lens=ql, kv_lens=kl, dout=do)
+
+    def loss():
+        return (ref.run(q, k, v, lam, causal, q_lens=ql, kv_lens=kl)["out"][0] * do).sum()
+
+    for x, name in ((q, "dq"), (k, "dk"), (v, "dv"), (lam, "dlam")):
+        for i in np.ndindex(x.shape):
+            old, eps = x[i], 1e-5
+            x[i] = old + eps
+            up = loss()
+            x[i] = old - eps
+            down = loss()
+            x[i] = old
+            assert abs((up - down) / (2 * eps) - got[name][0][i]) < 1e-8

@@ -1,0 +1,339 @@
+"""Differential attention on the GPU against the formulas in 64 bits: forward, gradients, lengths, layouts."""
+import numpy as np
+import pytest
+
+import diff_reference as ref
+import paper_2410_20926_b200 as ta
+
+pytestmark = pytest.mark.gpu
+
+
+def draw(seed, *shapes, dtype="bfloat16"):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    return [torch.randn(*s, device="cuda", generator=gen).to(getattr(torch, dtype)) for s in shapes]
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def ints(x):
+    import torch
+    return None if x is None else torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def lambdas(seed, n):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    return 0.1 + 0.8 * torch.rand(n, device="cuda", generator=gen)
+
+
+def near(name, got, want):
+    val, tol = want
+    err = np.abs(host(got) - val)
+    assert np.isfinite(host(got)).all(), name
+    # (the bounds are first order: a thousandth on top; nothing else)
+    assert (err <= 1.001 * tol).all(), (name, float(err.max()), float((err - 1.001 * tol).max()))
+
+
+def check(B, H, Hk, Nq, Nk, D, dtype="bfloat16", causal=True, ql=None, kl=None, scale=None, one_lambda=False, grad=True,
+          seed=0, flags=0):
+    """Forward through the C ABI (guard bands around the result), then the gradients."""
+    import torch
+    q, k, v, do = draw(seed, (B, H, Nq, D), (B, Hk, Nk, D), (B, Hk, Nk, D), (B, H, Nq, D), dtype=dtype)
+    lam = lambdas(seed + 1, 1 if one_lambda else H)
+    code = ta.TA_DTYPE_BF16 if dtype == "bfloat16" else ta.TA_DTYPE_F32
+    n, pad = B * H * Nq * D, 256
+    buf = torch.full((n + 2 * pad,), float("nan"), dtype=q.dtype, device="cuda")
+    out = buf[pad:pad + n].view(B, H, Nq, D)
+    saved = torch.empty(ta.ta_diff_workspace_bytes(B, H, Hk, Nq, Nk, D, code, ta.TA_DIFF_WS_SAVED), dtype=torch.uint8, device="cuda")
+    args = (B, H, Hk, Nq, Nk, D, causal)
+    kw = dict(dtype=code, softmax_scale=scale or 0.0, q_lens=ints(ql), kv_lens=ints(kl), flags=flags)
+    ta.ta_diff_forward(q, k, v, out, lam, lam.numel(), *args, saved=saved, **kw)
+    torch.cuda.synchronize()
+    ta.ta_device_status()
+    assert torch.isnan(buf[:pad]).all() and torch.isnan(buf[pad + n:]).all()
+    want = ref.run(host(q), host(k), host(v), host(lam), causal, q_lens=ql, kv_lens=kl, scale=scale,
+                   dout=host(do) if grad else None, bf16=dtype == "bfloat16")
+    near("out", out, want["out"])
+    if not grad:
+        return
+    dq, dk, dv, dlam = torch.full_like(q, float("nan")), torch.full_like(k, float("nan")), torch.full_like(v, float("nan")), torch.full_like(lam, float("nan"))
+    ta.ta_diff_backward(do, q, k, v, out, lam, lam.numel(), saved, dq, dk, dv, dlam, *args, **kw)
+    torch.cuda.synchronize()
+    ta.ta_device_status()
+    for name, got in (("dq", dq), ("dk", dk), ("dv", dv)):
+        near(name, got, want[name])
+    val, tol = want["dlam"]
+    near("dlam", dlam, (val.sum(keepdims=True), tol.sum(keepdims=True)) if one_lambda else (val, tol))
+
+
+SHAPES = [  # B, H, H_kv, Nq, Nk, D
+    (1, 1, 1, 1, 1, 2), (2, 2, 1, 5, 5, 6), (1, 4, 2, 64, 64, 64), (1, 2, 2, 65, 65, 128), (2, 3, 1, 130, 130, 64),
+    (1, 4, 1, 200, 200, 128), (1, 2, 1, 40, 90, 80), (1, 2, 2, 33, 33, 160), (1, 1, 1, 70, 70, 256), (1, 6, 2, 127, 300, 128),
+    (1, 2, 1, 300, 128, 64), (2, 8, 2, 3, 77, 128), (1, 4, 4, 1, 500, 64), (1, 16, 2, 1, 129, 128), (3, 4, 1, 8, 1000, 64),
+    (1, 2, 2, 257, 257, 128), (1, 2, 2, 384, 384, 64),
+]
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_matches_formula(shape, dtype, causal):
+    check(*shape, dtype=dtype, causal=causal)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("D", [64, 128, 80])
+def test_lengths(D, causal, dtype):
+    """Padded batches, empty sequences, rows before the first key, lengths beyond the tensors (clamped)."""
+    check(5, 2, 1, 150, 150, D, dtype=dtype, causal=causal, ql=[150, 1, 0, 131, 64], kl=[150, 1, 0, 131, 64])
+    check(5, 2, 2, 140, 200, D, dtype=dtype, causal=causal, ql=[140, 200, 100, 7, -3], kl=[40, 1000, 0, 130, 129])
+    check(4, 4, 2, 2, 300, D, dtype=dtype, causal=causal, ql=[2, 1, 2, 0], kl=[300, 129, 1, 17])
+    check(3, 4, 2, 1, 700, D, dtype=dtype, causal=causal, kl=[700, 0, 257])
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_scale_and_single_lambda(dtype):
+    check(2, 4, 2, 100, 100, 64, dtype=dtype, scale=0.3, one_lambda=True)
+    check(2, 4, 2, 1, 100, 128, dtype=dtype, scale=-0.05, one_lambda=True, causal=False)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_generic_kernels_on_request(D):
+    check(1, 4, 2, 150, 150, D, flags=ta.TA_FLAG_NO_TENSOR_CORE)
+    check(1, 4, 2, 1, 150, D, flags=ta.TA_FLAG_NO_TENSOR_CORE)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_peaked_rows(D):
+    """Scores that reach several hundred: running maxima that move at every key block, weights that vanish."""
+    import torch
+    q, k, v = draw(3, (1, 2, 300, D), (1, 1, 300, D), (1, 1, 300, D))
+    ramp = torch.linspace(0.2, 8.0, 300, device="cuda")[:, None]
+    q, k = (q * 4).bfloat16(), (k * ramp).bfloat16()
+    lam = lambdas(4, 2)
+    for causal in (False, True):
+        got = ta.differential_attention(q, k, v, lam, causal=causal)
+        near("out", got, ref.run(host(q), host(k), host(v), host(lam), causal)["out"])
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("D", [64, 128, 80])
+@pytest.mark.parametrize("Nq", [150, 2])
+def test_what_stands_behind_the_lengths_does_not_matter(Nq, D, dtype):
+    """NaN and infinities in the slots and rows that do not count; same results as with zeros there, bit for bit."""
+    import torch
+    B, H, Hk, Nk = 3, 4, 2, 200
+    ql, kl = [Nq, 1, Nq // 2], [140, 2, 200]
+    res = []
+    for junk in (0.0, float("nan"), float("inf")):
+        q, k, v, do = draw(5, (B, H, Nq, D), (B, Hk, Nk, D), (B, Hk, Nk, D), (B, H, Nq, D), dtype=dtype)
+        for b in range(B):
+            q[b, :, ql[b]:] = junk
+            do[b, :, ql[b]:] = junk
+            k[b, :, kl[b]:] = junk
+            v[b, :, kl[b]:] = junk
+        lam = lambdas(6, H)
+        t = [x.requires_grad_() for x in (q, k, v, lam)]
+        out = ta.differential_attention(*t, causal=True, q_lens=ints(ql), kv_lens=ints(kl))
+        res.append([out.detach()] + list(torch.autograd.grad(out, t, do)))
+    for other in res[1:]:
+        for a, b in zip(res[0], other):
+            assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
+def fused(seed, B, H, Hk, N, D, dtype, shift):
+    """q, k, v as views of one projection [B, N, (H + 2 H_kv) D], starting `shift` elements into it."""
+    (buf,) = draw(seed, (B, N, (H + 2 * Hk) * D + 16), dtype=dtype)
+    rows = buf[..., shift:shift + (H + 2 * Hk) * D].unflatten(-1, (H + 2 * Hk, D)).transpose(1, 2)
+    return rows[:, :H], rows[:, H:H + Hk], rows[:, H + Hk:]
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("N", [150, 2])
+def test_strided_and_unaligned_views(N, shift, dtype):
+    import torch
+    B, H, Hk, D = 2, 4, 2, 64
+    q, k, v = fused(7, B, H, Hk, N, D, dtype, shift)
+    lam = lambdas(8, H)
+    (do,) = draw(9, (B, N, H, D), dtype=dtype)
+    do = do.transpose(1, 2)
+    got = []
+    for make in (lambda x: x, lambda x: x.contiguous()):
+        t = [make(x).detach().requires_grad_() for x in (q, k, v)] + [lam.detach().requires_grad_()]
+        out = ta.differential_attention(*t)
+        got.append([out] + list(torch.autograd.grad(out, t, make(do))))
+    want = ref.run(host(q), host(k), host(v), host(lam), True, dout=host(do), bf16=dtype == "bfloat16")
+    for res in got:
+        for name, x in zip(("out", "dq", "dk", "dv", "dlam"), res):
+            near(name, x, want[name])
+    # a result in another layout, written through the C ABI
+    buf = torch.zeros(B, N, H, D, dtype=q.dtype, device="cuda").transpose(1, 2)
+    st = lambda x: x.stride()[:3]  # noqa: E731
+    ta.ta_diff_forward(q, k, v, buf, lam, H, B, H, Hk, N, N, D, True, q_strides=st(q), k_strides=st(k), v_strides=st(v),
+                       out_strides=st(buf), dtype=ta.TA_DTYPE_BF16 if dtype == "bfloat16" else ta.TA_DTYPE_F32)
+    assert torch.equal(buf, got[0][0])
+
+
+def test_expanded_inputs_and_summed_loss():
+    """One KV head for a whole batch (stride 0), and the gradient of a plain sum (all strides 0)."""
+    import torch
+    q, k, v = draw(10, (3, 2, 140, 64), (1, 1, 140, 64), (1, 1, 140, 64), dtype="float32")
+    lam = lambdas(11, 2)
+    t = [x.requires_grad_() for x in (q, k, v, lam)]
+    out = ta.differential_attention(q, k.expand(3, 1, 140, 64), v.expand(3, 1, 140, 64), lam)
+    out.sum().backward()
+    want = ref.run(host(q), np.repeat(host(k), 3, 0), np.repeat(host(v), 3, 0), host(lam), True, dout=np.ones(q.shape), bf16=False)
+    near("dq", q.grad, want["dq"])
+    for x, name in ((k, "dk"), (v, "dv")):
+        val, tol = want[name]
+        near(name, x.grad, (val.sum(0, keepdims=True), tol.sum(0, keepdims=True) + 4 * ref.U32 * np.abs(val).sum(0, keepdims=True)))
+    near("dlam", t[3].grad, want["dlam"])
+
+
+def test_bfloat16_expanded_keys():
+    q, k, v = draw(12, (3, 2, 140, 64), (1, 1, 140, 64), (1, 1, 140, 64))
+    lam = lambdas(13, 2)
+    got = ta.differential_attention(q, k.expand(3, 1, 140, 64), v.expand(3, 1, 140, 64), lam)
+    near("out", got, ref.run(host(q), np.repeat(host(k), 3, 0), np.repeat(host(v), 3, 0), host(lam), True)["out"])
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("Nq,Nk", [(300, 300), (1, 3000)])
+def test_repeats_bit_for_bit(Nq, Nk, dtype):
+    import torch
+    q, k, v, do = draw(14, (2, 8, Nq, 128), (2, 2, Nk, 128), (2, 2, Nk, 128), (2, 8, Nq, 128), dtype=dtype)
+    t = [x.requires_grad_() for x in (q, k, v, lambdas(15, 8))]
+    first = None
+    for _ in range(3):
+        out = ta.differential_attention(*t)
+        res = [out.detach()] + list(torch.autograd.grad(out, t, do))
+        first = first or res
+        assert all(torch.equal(a, b) for a, b in zip(first, res))
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("Nq,Nk", [(200, 200), (1, 1000)])
+def test_captured_and_replayed_on_new_inputs(Nq, Nk, dtype):
+    """Forward and backward through the C ABI in one graph, on memory of the library's pool and the caller's; two graphs
+    captured from the same buffers and replayed in turn."""
+    import torch
+    B, H, Hk, D = 2, 4, 2, 64
+    code = ta.TA_DTYPE_BF16 if dtype == "bfloat16" else ta.TA_DTYPE_F32
+    q, k, v, do = draw(16, (B, H, Nq, D), (B, Hk, Nk, D), (B, Hk, Nk, D), (B, H, Nq, D), dtype=dtype)
+    lam, kl = lambdas(17, H), ints([Nk, Nk - 50])
+    out, dq, dk, dv, dlam = torch.empty_like(q), torch.empty_like(q), torch.empty_like(k), torch.empty_like(v), torch.empty_like(lam)
+    saved = torch.empty(ta.ta_diff_workspace_bytes(B, H, Hk, Nq, Nk, D, code, ta.TA_DIFF_WS_SAVED), dtype=torch.uint8, device="cuda")
+
+    def call():
+        ta.ta_diff_forward(q, k, v, out, lam, H, B, H, Hk, Nq, Nk, D, True, dtype=code, kv_lens=kl, saved=saved)
+        ta.ta_diff_backward(do, q, k, v, out, lam, H, saved, dq, dk, dv, dlam, B, H, Hk, Nq, Nk, D, True, dtype=code, kv_lens=kl)
+
+    call()
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    for g in graphs:
+        with torch.cuda.graph(g):
+            call()
+    for i, g in enumerate(graphs * 2):
+        for x, y in zip((q, k, v, do), draw(18 + i, q.shape, k.shape, v.shape, q.shape, dtype=dtype)):
+            x.copy_(y)
+        lam.copy_(lambdas(30 + i, H))
+        kl.copy_(ints([Nk - 7 * i, Nk - 51 + i]))
+        g.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in (out, dq, dk, dv, dlam)]
+        call()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, (out, dq, dk, dv, dlam)))
+
+
+def test_two_streams_at_once():
+    import torch
+    sets = [draw(40 + i, (2, 4, 1, 128), (2, 2, 2000, 128), (2, 2, 2000, 128)) + [lambdas(50 + i, 4)] for i in range(2)]
+    want = [ta.differential_attention(*s) for s in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(10):
+        got = []
+        for s, st in zip(sets, streams):
+            with torch.cuda.stream(st):
+                got.append(ta.differential_attention(*s))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_binding_refuses():
+    import torch
+    q, k, v = draw(60, (1, 4, 8, 64), (1, 2, 8, 64), (1, 2, 8, 64))
+    lam = lambdas(61, 4)
+    good = dict(q_lens=ints([8]), kv_lens=ints([8]))
+    ta.differential_attention(q, k, v, lam, **good)
+    for bad in (dict(q=q[0]), dict(k=k[:, :, :, :32]), dict(v=v[:, :, :7]), dict(k=k.float()), dict(lam=lam.double()),
+                dict(lam=lam[:3]), dict(lam=lam.cpu()), dict(q=q.half()), dict(q=q[:, :, :0]), dict(kv_lens=ints([8]).long()),
+                dict(q_lens=ints([8, 8])), dict(kv_lens=torch.tensor([8], dtype=torch.int32))):
+        kw = dict(dict(q=q, k=k, v=v, lam=lam), **bad)
+        with pytest.raises(ValueError):
+            ta.differential_attention(**kw)
+    with pytest.raises(ta.TaError):
+        ta.differential_attention(q[:, :3], k, v, lam[:3])           # 3 query heads, 2 KV heads
+
+
+def test_decoding_run_with_rotary_and_cache():
+    """A prompt, then tokens one by one against a cache: rotary positions on three axes and differential attention, as a
+    model would call them; every step equals the row of a pass over all tokens."""
+    import torch
+    B, H, Hk, D, N0, steps, slots = 2, 4, 2, 128, 37, 6, 64
+    N = N0 + steps
+    sec = (8, 12, 12)
+    q, k, v = draw(70, (B, H, N, D), (B, Hk, N, D), (B, Hk, N, D))
+    pos = torch.randint(0, 4000, (3, B, N), device="cuda", dtype=torch.int32)
+    lam = lambdas(71, H)
+    rq, rk = ta.multi_axis_rotary(q, k, sec, positions=pos, parts=2)
+    full = ta.differential_attention(rq, rk, v, lam)
+    near("out", full, ref.run(host(rq), host(rk), host(v), host(lam), True)["out"])
+    kc = torch.full((B, Hk, slots, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+    vc = kc.clone()
+    fill = torch.full((B,), N0, dtype=torch.int32, device="cuda")
+    pq, pk = ta.multi_axis_rotary(q[:, :, :N0], k[:, :, :N0], sec, positions=pos[:, :, :N0], parts=2)
+    kc[:, :, :N0], vc[:, :, :N0] = pk, v[:, :, :N0]
+    outs = [ta.differential_attention(pq, kc, vc, lam, kv_lens=fill)]
+    for t in range(N0, N):
+        sq, sk = ta.multi_axis_rotary(q[:, :, t:t + 1], k[:, :, t:t + 1], sec, positions=pos[:, :, t:t + 1], parts=2)
+        kc[:, :, t:t + 1], vc[:, :, t:t + 1] = sk, v[:, :, t:t + 1]
+        fill += 1
+        outs.append(ta.differential_attention(sq, kc, vc, lam, kv_lens=fill))
+    got = torch.cat(outs, 2)
+    near("decoded", got, ref.run(host(rq), host(rk), host(v), host(lam), True)["out"])
+
+
+def test_training_run_with_rotary():
+    """Gradients of the projections' outputs through rotary positions and differential attention together, against the
+    chain of the two references."""
+    import torch
+    from rotary_reference import angles, coordinates, rotate
+    B, H, Hk, D, dims, sec = 1, 4, 2, 64, (6, 25), (7, 9)
+    N = 150
+    q, k, v, do = draw(72, (B, H, N, D), (B, Hk, N, D), (B, Hk, N, D), (B, H, N, D), dtype="float32")
+    lam = lambdas(73, H)
+    t = [x.requires_grad_() for x in (q, k, v, lam)]
+    rq, rk = ta.multi_axis_rotary(q, k, sec, dims=dims, parts=2, per_axis_ladder=True)
+    out = ta.differential_attention(rq, rk, v, lam)
+    grads = torch.autograd.grad(out, t, do)
+    ang = angles(coordinates(dims, N)[:, None], sec, 10000.0, True)
+    want = ref.run(rotate(host(q), ang, 2, False), rotate(host(k), ang, 2, False), host(v), host(lam), True, dout=host(do), bf16=False)
+    for name, x, g in (("dq", q, grads[0]), ("dk", k, grads[1])):
+        val, tol = want[name]
+        # turned back, a pair's tolerance is at most the sum of both; the rotations' own roundings (of q, k before: 8 steps
+        # of the scores, of the gradient after: 8 steps) stay below as many again
+        both = tol.reshape(*tol.shape[:3], 2, D // 2)
+        i = np.arange(16)
+        pair = both[..., i] + both[..., i + 16]
+        both = np.concatenate([pair, pair], -1).reshape(tol.shape)
+        near(name, g, (rotate(val, ang, 2, False, inverse=True), 2 * both + 16 * ref.U32 * np.abs(val).max()))
+    near("dv", grads[2], (want["dv"][0], 2 * want["dv"][1]))
+    near("dlam", grads[3], (want["dlam"][0], 2 * want["dlam"][1]))
