@@ -413,7 +413,7 @@ typedef struct ta_diff_params {
     long long q_strides[3], k_strides[3], v_strides[3], out_strides[3]; /* elements between batch    */
                                /* entries, heads, tokens; all 0: contiguous.  D is always innermost   */
     void *saved;               /* device, 256-byte aligned, TA_DIFF_WS_SAVED bytes, or NULL: what     */
-                               /* ta_diff_backward needs of this pass (row statistics, A_2 V)         */
+                               /* ta_diff_backward needs of this pass (row statistics, A_1 V, A_2 V)  */
     void *workspace;           /* device, 256-byte aligned, TA_DIFF_WS_FORWARD bytes, or NULL: taken  */
     size_t workspace_bytes;    /* from the library's memory pool in stream order                      */
     unsigned flags;            /* TA_FLAG_NO_TENSOR_CORE or 0                                        */

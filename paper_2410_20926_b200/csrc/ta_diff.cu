@@ -51,14 +51,26 @@ int head_chunks(int B, int H, int H_kv, int Nk, int tile) {
 }
 
 struct SavedLayout {
-    size_t lse, o2, total;
+    size_t lse, step, o, total;
 };
 SavedLayout saved_layout(int B, int H, int Nq, int D, int dtype) {
     SavedLayout L;
+    const size_t rows = (size_t)B * H * Nq;
     L.lse = 0;
-    L.o2 = up256((size_t)B * H * Nq * sizeof(float2));
-    L.total = L.o2 + up256((size_t)B * H * Nq * D * elem_bytes(dtype));
+    L.step = up256(rows * sizeof(float2));
+    L.o = L.step + (dtype == TA_DTYPE_F32 ? 0 : up256(rows * sizeof(float2)));
+    L.total = L.o + up256(rows * D * 4);             // fp32: one value, bf16: two 16-bit ones
     return L;
+}
+void set_saved(DiffProblem *d, void *saved) {
+    const SavedLayout L = saved_layout(d->B, d->H, d->Nq, d->D, d->dtype);
+    d->lse = (float2 *)((char *)saved + L.lse);
+    if (d->dtype == TA_DTYPE_F32) {
+        d->o2 = (float *)((char *)saved + L.o);
+    } else {
+        d->ostep = (float2 *)((char *)saved + L.step);
+        d->o16 = (short *)((char *)saved + L.o);
+    }
 }
 
 size_t forward_bytes(int B, int H, int H_kv, int Nq, int Nk, int D) {
@@ -134,6 +146,18 @@ int check_common(const float *lambda, int lambda_count, int H, float scale, unsi
     return TA_OK;
 }
 
+// Whether the tensor-core kernels can address a tensor through a tensor map: rows on 16-byte boundaries, every stride
+// positive (an expanded dimension has stride 0) and below the map's 2^40 bytes.
+bool tma_ok(const void *p, const Strides3 &s, int B, int heads, int N) {
+    auto fine = [](long long x, int n) { return n == 1 || (x > 0 && x % 8 == 0 && x < (1ll << 39)); };
+    return (uintptr_t)p % 16 == 0 && fine(s.b, B) && fine(s.h, heads) && fine(s.n, N);
+}
+// Tensor cores: bf16 at the head dims whose tiles are whole 128-byte rows, and a positive scale (the kernels take the
+// row maximum of the unscaled scores).
+bool tc_shape(int D, int dtype, float scale, unsigned flags) {
+    return dtype == TA_DTYPE_BF16 && (D == 64 || D == 128) && scale > 0.f && !(flags & TA_FLAG_NO_TENSOR_CORE);
+}
+
 const long long kContiguous[3] = {0, 0, 0};
 
 int forward_impl(const ta_diff_params &p) {
@@ -161,13 +185,14 @@ int forward_impl(const ta_diff_params &p) {
     d.causal = p.causal ? 1 : 0; d.dtype = p.dtype;
     d.scale = p.softmax_scale != 0.f ? p.softmax_scale : 1.0f / sqrtf((float)(p.D / 2));
     d.q_lens = p.q_lens; d.kv_lens = p.kv_lens;
-    if (p.saved) {
-        const SavedLayout L = saved_layout(p.B, p.H, p.Nq, p.D, p.dtype);
-        d.lse = (float2 *)((char *)p.saved + L.lse);
-        d.o2 = (char *)p.saved + L.o2;
-    }
+    if (p.saved) set_saved(&d, p.saved);
     d.stream = (cudaStream_t)p.stream;
-    if (!few_rows(p.H, p.H_kv, p.Nq)) return launch_diff_simt(d);
+    if (!few_rows(p.H, p.H_kv, p.Nq)) {
+        const bool tc = tc_shape(d.D, d.dtype, d.scale, p.flags) && tma_ok(d.q, d.sq, d.B, d.H, d.Nq) &&
+                        tma_ok(d.k, d.sk, d.B, d.H_kv, d.Nk) && tma_ok(d.v, d.sv, d.B, d.H_kv, d.Nk) &&
+                        tma_ok(d.out, d.so, d.B, d.H, d.Nq);
+        return tc ? launch_diff_tc(d) : launch_diff_simt(d);
+    }
     char *ws = (char *)p.workspace;
     PooledGuard pooled{nullptr, d.stream};
     if (!ws) {
@@ -211,9 +236,7 @@ int backward_impl(const ta_diff_bwd_params &p) {
     d.causal = p.causal ? 1 : 0; d.dtype = p.dtype;
     d.scale = p.softmax_scale != 0.f ? p.softmax_scale : 1.0f / sqrtf((float)(p.D / 2));
     d.q_lens = p.q_lens; d.kv_lens = p.kv_lens;
-    const SavedLayout S = saved_layout(p.B, p.H, p.Nq, p.D, p.dtype);
-    d.lse = (float2 *)((char *)const_cast<void *>(p.saved) + S.lse);
-    d.o2 = (char *)const_cast<void *>(p.saved) + S.o2;
+    set_saved(&d, const_cast<void *>(p.saved));
     d.stream = (cudaStream_t)p.stream;
     char *ws = (char *)p.workspace;
     PooledGuard pooled{nullptr, d.stream};

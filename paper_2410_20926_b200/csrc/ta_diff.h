@@ -23,7 +23,13 @@ struct DiffProblem {
     float scale;
     const int *q_lens, *kv_lens;
     float2 *lse;                 // [B*H*Nq]: log2 of the sum of 2^(score * scale * log2 e), per map; +inf: row sees no key
-    void *o2;                    // [B,H,Nq,D] contiguous: A_2 V, dtype
+    // What the backward needs of A_1 V and A_2 V (its d_c = <dout, A_c V>).  fp32: A_2 V itself, [B*H*Nq][D].  bf16: both, as
+    // 16-bit whole numbers times a step per row (the row's largest magnitude / 32767), [B*H*Nq][2][D]: as many bits as
+    // bf16, but off by 2^-16 of the row's largest value instead of 2^-8 of each, which rows that see few keys, where
+    // d_c nearly cancels dA, would hand on to dQ and dK.
+    float *o2;
+    short *o16;
+    float2 *ostep;
     cudaStream_t stream;
 };
 
@@ -42,6 +48,12 @@ __device__ __forceinline__ DiffSpan diff_span(const int *q_lens, const int *kv_l
     s.kl = kv_lens ? min(max(__ldg(kv_lens + b), 0), Nk) : Nk;
     s.off = s.kl - s.ql;
     return s;
+}
+
+// step of a row with largest magnitude `most`, and the whole number for x
+__device__ __forceinline__ float diff_inv_step(float most) { return most > 0.f ? 32767.f / most : 0.f; }
+__device__ __forceinline__ uint32_t diff_pack16(float a, float b) {
+    return ((uint32_t)__float2int_rn(a) & 0xFFFFu) | ((uint32_t)__float2int_rn(b) << 16);
 }
 
 // Buffers of one call behind the forward's workspace: partial results of `splits` key ranges per query row,
@@ -74,5 +86,7 @@ int launch_diff_stats(const DiffProblem &p, float4 *stats);
 int launch_diff_simt_bwd(const DiffProblem &p, const DiffGrads &g);
 int launch_diff_group_sum(const DiffProblem &p, const DiffGrads &g);
 int launch_diff_dlambda(const DiffProblem &p, const DiffGrads &g, int tiles, float *dlambda);
+// tensor cores: bf16, D = 64 or 128, 16-byte aligned rows (ta_diff_tc.cu)
+int launch_diff_tc(const DiffProblem &p);
 
 }  // namespace ta

@@ -211,15 +211,37 @@ diff_simt_kernel(const __grid_constant__ SimtArgs a) {
         const float i1 = any ? 1.f / l[0][i] : 0.f, i2 = any ? 1.f / l[1][i] : 0.f;
         T *orow = (T *)p.out + b * p.so.b + h * p.so.h + t * p.so.n;
         const long long row = (long long)bh * p.Nq + t;
+        float most1 = 0.f, most2 = 0.f;
+        if (p.o16) {
+#pragma unroll
+            for (int ch = 0; ch < C::kCh; ++ch)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    most1 = fmaxf(most1, fabsf(comp(o[0][ch][i], e)));
+                    most2 = fmaxf(most2, fabsf(comp(o[1][ch][i], e)));
+                }
+            const unsigned half_warp = 0xFFFFu << (threadIdx.x & 16);
+#pragma unroll
+            for (int w = 8; w > 0; w >>= 1) {
+                most1 = fmaxf(most1, __shfl_xor_sync(half_warp, most1, w));
+                most2 = fmaxf(most2, __shfl_xor_sync(half_warp, most2, w));
+            }
+            if (tx == 0) p.ostep[row] = make_float2(most1 * i1 * (1.f / 32767.f), most2 * i2 * (1.f / 32767.f));
+        }
+        const float n1 = diff_inv_step(most1), n2 = diff_inv_step(most2);
 #pragma unroll
         for (int ch = 0; ch < C::kCh; ++ch)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int c = real_col<DT>(4 * tx + 64 * ch + e, p.D);
                 if (c < 0) continue;
-                const float o2 = comp(o[1][ch][i], e) * i2;
-                store1(orow + c, comp(o[0][ch][i], e) * i1 - lam * o2);
-                if (p.o2) store1((T *)p.o2 + row * p.D + c, o2);
+                const float o1 = comp(o[0][ch][i], e), o2 = comp(o[1][ch][i], e);
+                store1(orow + c, o1 * i1 - lam * (o2 * i2));
+                if (p.o2) p.o2[row * p.D + c] = o2 * i2;
+                if (p.o16) {
+                    p.o16[row * 2 * p.D + c] = (short)__float2int_rn(o1 * n1);
+                    p.o16[row * 2 * p.D + p.D + c] = (short)__float2int_rn(o2 * n2);
+                }
             }
         if (p.lse && tx == 0)
             p.lse[row] = any ? make_float2(m[0][i] + log2f(l[0][i]), m[1][i] + log2f(l[1][i])) : make_float2(INFINITY, INFINITY);
@@ -418,13 +440,32 @@ diff_combine_kernel(const __grid_constant__ SimtArgs a) {
     const float lam = __ldg(p.lambda + (p.lambda_count > 1 ? h : 0));
     const float i1 = any ? 1.f / l1 : 0.f, i2 = any ? 1.f / l2 : 0.f;
     T *orow = (T *)p.out + b * p.so.b + h * p.so.h + (long long)t * p.so.n;
+    float most1 = 0.f, most2 = 0.f;
+    if (p.o16) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            most1 = fmaxf(most1, fabsf(acc1[i]));
+            most2 = fmaxf(most2, fabsf(acc2[i]));
+        }
+#pragma unroll
+        for (int w = 16; w > 0; w >>= 1) {
+            most1 = fmaxf(most1, __shfl_xor_sync(0xffffffffu, most1, w));
+            most2 = fmaxf(most2, __shfl_xor_sync(0xffffffffu, most2, w));
+        }
+        if (lane == 0) p.ostep[row] = make_float2(most1 * i1 * (1.f / 32767.f), most2 * i2 * (1.f / 32767.f));
+    }
+    const float n1 = diff_inv_step(most1), n2 = diff_inv_step(most2);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int c = lane + 32 * i;
         if (c >= D) break;
         const float o2 = acc2[i] * i2;
         store1(orow + c, acc1[i] * i1 - lam * o2);
-        if (p.o2) store1((T *)p.o2 + row * D + c, o2);
+        if (p.o2) p.o2[row * D + c] = o2;
+        if (p.o16) {
+            p.o16[row * 2 * D + c] = (short)__float2int_rn(acc1[i] * n1);
+            p.o16[row * 2 * D + D + c] = (short)__float2int_rn(acc2[i] * n2);
+        }
     }
     if (p.lse && lane == 0)
         p.lse[row] = any ? make_float2(m1 + log2f(l1), m2 + log2f(l2)) : make_float2(INFINITY, INFINITY);
@@ -432,7 +473,7 @@ diff_combine_kernel(const __grid_constant__ SimtArgs a) {
 
 // ------------------------------------------------------------------ backward
 
-// One warp per row: d_2 = <dout, A_2 V>, d_1 = <dout, A_1 V> = <dout, out> + lambda d_2.
+// One warp per row: d_c = <dout, A_c V>; in fp32 d_1 = <dout, out> + lambda d_2.
 template <typename T>
 __global__ void __launch_bounds__(128)
 diff_stats_kernel(const __grid_constant__ SimtArgs a, float4 *stats) {
@@ -442,24 +483,39 @@ diff_stats_kernel(const __grid_constant__ SimtArgs a, float4 *stats) {
     const int bh = (int)(idx / a.prow), t = (int)(idx - bh * a.prow);
     if (bh >= p.B * p.H) return;
     const int b = bh / p.H, h = bh - b * p.H;
+    const long long row = (long long)bh * p.Nq + t;
     float2 lse = make_float2(INFINITY, INFINITY);
     float d1 = 0.f, d2 = 0.f;
-    if (t < p.Nq) lse = p.lse[(long long)bh * p.Nq + t];
+    if (t < p.Nq) lse = p.lse[row];
     if (lse.x < INFINITY) {
         const T *g = (const T *)p.dout + b * p.sdo.b + h * p.sdo.h + (long long)t * p.sdo.n;
-        const T *o = (const T *)p.out + b * p.so.b + h * p.so.h + (long long)t * p.so.n;
-        const T *o2 = (const T *)p.o2 + ((long long)bh * p.Nq + t) * p.D;
-        for (int c = lane; c < p.D; c += 32) {
-            const float x = load1(g + c);
-            d1 = fmaf(x, load1(o + c), d1);
-            d2 = fmaf(x, load1(o2 + c), d2);
+        if constexpr (sizeof(T) == 4) {
+            const T *o = (const T *)p.out + b * p.so.b + h * p.so.h + (long long)t * p.so.n;
+            for (int c = lane; c < p.D; c += 32) {
+                const float x = load1(g + c);
+                d1 = fmaf(x, load1(o + c), d1);
+                d2 = fmaf(x, p.o2[row * p.D + c], d2);
+            }
+        } else {
+            const short *o = p.o16 + row * 2 * p.D;
+            for (int c = lane; c < p.D; c += 32) {
+                const float x = load1(g + c);
+                d1 = fmaf(x, (float)o[c], d1);
+                d2 = fmaf(x, (float)o[p.D + c], d2);
+            }
         }
 #pragma unroll
         for (int w = 16; w > 0; w >>= 1) {
             d1 += __shfl_xor_sync(0xffffffffu, d1, w);
             d2 += __shfl_xor_sync(0xffffffffu, d2, w);
         }
-        d1 = fmaf(__ldg(p.lambda + (p.lambda_count > 1 ? h : 0)), d2, d1);
+        if constexpr (sizeof(T) == 4) {
+            d1 = fmaf(__ldg(p.lambda + (p.lambda_count > 1 ? h : 0)), d2, d1);
+        } else {
+            const float2 step = p.ostep[row];
+            d1 *= step.x;
+            d2 *= step.y;
+        }
     }
     if (lane == 0) stats[idx] = make_float4(lse.x, lse.y, d1, d2);
 }

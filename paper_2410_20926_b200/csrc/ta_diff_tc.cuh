@@ -1,0 +1,71 @@
+// Pieces shared by the tensor-core kernels of differential attention.
+#pragma once
+
+#include "ta_diff.h"
+#include "ta_ptx.cuh"
+
+namespace ta {
+namespace {
+
+// Map c of a tile whose rows hold [first half | second half] of the features in 128-byte swizzled slabs of 64: where its
+// K-major k-step kb (16 features) starts, and where its features start for an operand read feature-major.
+template <int D>
+__device__ __forceinline__ constexpr uint32_t map_k_off(int c, int kb, uint32_t slab_bytes) {
+    return D == 128 ? (uint32_t)c * slab_bytes + (uint32_t)kb * 32u : (uint32_t)c * 64u + (uint32_t)kb * 32u;
+}
+template <int D>
+__device__ __forceinline__ constexpr uint32_t map_n_off(int c, uint32_t slab_bytes) {
+    return D == 128 ? (uint32_t)c * slab_bytes : (uint32_t)c * 64u;
+}
+
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n .reg .b64 x, y, z, w;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n mov.b64 z, {%6, %7};\n"
+        " fma.rn.f32x2 w, x, y, z;\n mov.b64 {%0, %1}, w;\n}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n .reg .b64 x, y, w;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n"
+        " add.rn.f32x2 w, x, y;\n mov.b64 {%0, %1}, w;\n}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n .reg .b64 x, y, w;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n"
+        " mul.rn.f32x2 w, x, y;\n mov.b64 {%0, %1}, w;\n}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t *v) {
+    __syncwarp();
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+          "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]),
+          "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
+          "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+        : "memory");
+}
+
+// Zeroes rows [r0, r1) of a tile in shared memory (kSlabs slabs of 128-byte rows); the whole warp takes part.  For rows the
+// tensor holds but the call's lengths do not count: whatever stands there must not meet a weight of 0 in a product.
+__device__ __forceinline__ void zero_rows(uint32_t tile, uint32_t slab_bytes, int slabs, int r0, int r1) {
+    const int lane = threadIdx.x & 31;
+    for (int s = 0; s < slabs; ++s)
+        for (int i = r0 * 8 + lane; i < r1 * 8; i += 32) st_shared_v4(tile + s * slab_bytes + (uint32_t)i * 16u, 0, 0, 0, 0);
+}
+
+// warp-uniform bounded wait of a whole warp
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, uint32_t where, volatile uint32_t *abort_flag) {
+    const bool ok = mbar_wait_abortable(bar, parity, where, abort_flag);
+    return __all_sync(0xffffffffu, ok);
+}
+
+}  // namespace
+}  // namespace ta

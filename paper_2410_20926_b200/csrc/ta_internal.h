@@ -211,12 +211,16 @@ int make_hop_map(CUtensorMap *map, const void *base, int heads_total, int N, int
 int make_view_map(CUtensorMap *map, const void *base, int heads_total, int N, int D, const HopDesc &hd, int elem,
                   int box_t, int box_inner, int box_outer);
 
+// Map of a strided [B][heads][N][D] bf16 tensor (ta_tc.cu).
+int make_strided_map(CUtensorMap *map, const void *base, const long long *strides, int B, int heads, int N, int D, int box_rows);
+
 // Device error words (bounded waits that expired), one per tensor-core translation unit:
 // copies the word to *word and clears it.
 int read_status_tc_forward(unsigned int *word);
 int read_status_tc_backward(unsigned int *word);
 int read_status_tc_fused(unsigned int *word);
 int read_status_tc_backward_long(unsigned int *word);
+int read_status_diff_tc(unsigned int *word);
 
 // CUDA error code seen by the last call of this host thread that returned TA_ERR_CUDA.
 extern thread_local int tl_last_cuda_error;

@@ -554,6 +554,40 @@ int make_view_map(CUtensorMap *map, const void *base, int heads_total, int N, in
     return TA_OK;
 }
 
+// Rank-5 map (D, token, 1, head, batch) of a strided bf16 tensor [B][heads][N][D]; strides in elements (batch, head, token),
+// multiples of 8; box: 64 features of `box_rows` tokens of one head, 128-byte swizzle.
+int make_strided_map(CUtensorMap *map, const void *base, const long long *strides, int B, int heads, int N, int D, int box_rows) {
+    EncodeTiledFn enc = encode_fn();
+    if (!enc) {
+        tl_last_cuda_error = -1000;
+        return TA_ERR_CUDA;
+    }
+    // (the stride of a dimension of extent 1 is never used: any valid one does)
+    const cuuint64_t row = N > 1 ? (cuuint64_t)strides[2] * 2 : (cuuint64_t)D * 2;
+    const cuuint64_t head = heads > 1 ? (cuuint64_t)strides[1] * 2 : row;
+    const cuuint64_t batch = B > 1 ? (cuuint64_t)strides[0] * 2 : row;
+    cuuint64_t gdim[5] = {(cuuint64_t)D, (cuuint64_t)N, 1, (cuuint64_t)heads, (cuuint64_t)B};
+    cuuint64_t gstr[4] = {row, row, head, batch};
+    cuuint32_t box[5] = {64u, (cuuint32_t)box_rows, 1u, 1u, 1u};
+    cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+    if (!thread_has_context()) cudaFree(nullptr);   // (see make_view_map)
+    auto encode = [&] {
+        return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(base), gdim, gstr, box, estr,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    };
+    CUresult r = encode();
+    if (r == CUDA_ERROR_INVALID_CONTEXT) {
+        cudaFree(nullptr);
+        r = encode();
+    }
+    if (r != CUDA_SUCCESS) {
+        tl_last_cuda_error = -1000 - (int)r;
+        return TA_ERR_CUDA;
+    }
+    return TA_OK;
+}
+
 namespace {
 
 template <int D>

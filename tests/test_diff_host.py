@@ -65,7 +65,7 @@ def test_struct_sizes_are_checked():
 def test_workspace_bytes():
     up = lambda x: (x + 255) // 256 * 256  # noqa: E731
     size = ta.ta_diff_workspace_bytes
-    assert size(2, 4, 2, 100, 100, 64, ta.TA_DTYPE_BF16, ta.TA_DIFF_WS_SAVED) == up(800 * 8) + up(800 * 64 * 2)
+    assert size(2, 4, 2, 100, 100, 64, ta.TA_DTYPE_BF16, ta.TA_DIFF_WS_SAVED) == 2 * up(800 * 8) + up(800 * 64 * 4)
     assert size(2, 4, 2, 100, 100, 64, ta.TA_DTYPE_F32, ta.TA_DIFF_WS_SAVED) == up(800 * 8) + up(800 * 64 * 4)
     assert size(2, 4, 2, 1, 100, 64) > 0                       # few rows: partial sums
     assert size(2, 4, 2, 100, 100, 64, mode=ta.TA_DIFF_WS_BACKWARD) >= 8 * 128 * 16
