@@ -81,18 +81,23 @@ size_t forward_bytes(int B, int H, int H_kv, int Nq, int Nk, int D) {
 
 struct BackwardLayout {
     size_t stats, dlam, part, total;
-    int q_tile, k_tile, hsplit;
+    int hsplit, dlam_parts;
 };
 BackwardLayout backward_layout(int B, int H, int H_kv, int Nq, int Nk, int D, bool tc) {
     BackwardLayout L;
-    L.q_tile = L.k_tile = diff_simt_tile(D);
-    (void)tc;
-    L.hsplit = head_chunks(B, H, H_kv, Nk, L.k_tile);
+    const int tile = tc ? 128 : diff_simt_tile(D);
+    L.hsplit = head_chunks(B, H, H_kv, Nk, tile);
+    L.dlam_parts = (Nq + tile - 1) / tile * (tc ? 8 : 1);
     L.stats = 0;
     L.dlam = up256((size_t)B * H * diff_padded_rows(Nq) * sizeof(float4));
-    L.part = L.dlam + up256((size_t)B * H * ((Nq + L.q_tile - 1) / L.q_tile) * sizeof(float));
+    L.part = L.dlam + up256((size_t)B * H * L.dlam_parts * sizeof(float));
     L.total = L.part + (L.hsplit > 1 ? up256((size_t)2 * L.hsplit * B * H_kv * Nk * D * sizeof(float)) : 0);
     return L;
+}
+// (which kernels run also depends on the addresses: the workspace is large enough for either)
+size_t backward_bytes(int B, int H, int H_kv, int Nq, int Nk, int D) {
+    const size_t x = backward_layout(B, H, H_kv, Nq, Nk, D, true).total, y = backward_layout(B, H, H_kv, Nq, Nk, D, false).total;
+    return x > y ? x : y;
 }
 
 Strides3 strides_of(const long long *given, int heads, int N, int D) {
@@ -220,8 +225,7 @@ int backward_impl(const ta_diff_bwd_params &p) {
                          {p.dout, p.dout_strides, p.H, p.Nq, false}, {p.dq, kContiguous, p.H, p.Nq, true},
                          {p.dk, kContiguous, p.H_kv, p.Nk, true}, {p.dv, kContiguous, p.H_kv, p.Nk, true}};
     if ((rc = check_tensors(t, 8, p.B, p.D, elem)) != TA_OK) return rc;
-    const BackwardLayout L = backward_layout(p.B, p.H, p.H_kv, p.Nq, p.Nk, p.D, false);
-    if (p.workspace && p.workspace_bytes < L.total) return TA_ERR_WORKSPACE;
+    if (p.workspace && p.workspace_bytes < backward_bytes(p.B, p.H, p.H_kv, p.Nq, p.Nk, p.D)) return TA_ERR_WORKSPACE;
     if ((rc = check_arch()) != TA_OK) return rc;
 
     DiffProblem d = {};
@@ -238,6 +242,10 @@ int backward_impl(const ta_diff_bwd_params &p) {
     d.q_lens = p.q_lens; d.kv_lens = p.kv_lens;
     set_saved(&d, const_cast<void *>(p.saved));
     d.stream = (cudaStream_t)p.stream;
+    const bool tc = tc_shape(d.D, d.dtype, d.scale, p.flags) && tma_ok(d.q, d.sq, d.B, d.H, d.Nq) &&
+                    tma_ok(d.k, d.sk, d.B, d.H_kv, d.Nk) && tma_ok(d.v, d.sv, d.B, d.H_kv, d.Nk) &&
+                    tma_ok(d.dout, d.sdo, d.B, d.H, d.Nq);
+    const BackwardLayout L = backward_layout(d.B, d.H, d.H_kv, d.Nq, d.Nk, d.D, tc);
     char *ws = (char *)p.workspace;
     PooledGuard pooled{nullptr, d.stream};
     if (!ws) {
@@ -251,9 +259,9 @@ int backward_impl(const ta_diff_bwd_params &p) {
     g.hsplit = L.hsplit;
     g.dlam_part = (float *)(ws + L.dlam);
     if ((rc = launch_diff_stats(d, (float4 *)(ws + L.stats))) != TA_OK) return rc;
-    if ((rc = launch_diff_simt_bwd(d, g)) != TA_OK) return rc;
+    if ((rc = tc ? launch_diff_tc_bwd(d, g) : launch_diff_simt_bwd(d, g)) != TA_OK) return rc;
     if (g.hsplit > 1 && (rc = launch_diff_group_sum(d, g)) != TA_OK) return rc;
-    return launch_diff_dlambda(d, g, (p.Nq + L.q_tile - 1) / L.q_tile, p.dlambda);
+    return launch_diff_dlambda(d, g, L.dlam_parts, p.dlambda);
 }
 
 int finish(int rc) {
@@ -284,7 +292,7 @@ size_t ta_diff_workspace_bytes(int B, int H, int H_kv, int Nq, int Nk, int D, in
     if (check_shape(B, H, H_kv, Nq, Nk, D, dtype) != TA_OK) return 0;
     if (mode == TA_DIFF_WS_FORWARD) return forward_bytes(B, H, H_kv, Nq, Nk, D);
     if (mode == TA_DIFF_WS_SAVED) return saved_layout(B, H, Nq, D, dtype).total;
-    if (mode == TA_DIFF_WS_BACKWARD) return backward_layout(B, H, H_kv, Nq, Nk, D, false).total;
+    if (mode == TA_DIFF_WS_BACKWARD) return backward_bytes(B, H, H_kv, Nq, Nk, D);
     return 0;
 }
 

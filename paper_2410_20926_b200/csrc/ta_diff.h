@@ -74,7 +74,8 @@ struct DiffGrads {
     void *dq, *dk, *dv;          // contiguous, dtype
     float *part;                 // dK, dV partials [2][hsplit][B*H_kv*Nk*D] when hsplit > 1
     int hsplit;                  // items a GQA group's query heads are split over
-    float *dlam_part;            // [B*H][q tiles of the kernel in use]: sums of A_2 o dA
+    float *dlam_part;            // [B*H][parts]: sums of A_2 o dA; the tensor-core kernel writes 8 per query tile of 128, the
+                                 // generic one 1 per tile
 };
 
 // generic CUDA-core kernels (ta_diff_simt.cu)
@@ -88,5 +89,6 @@ int launch_diff_group_sum(const DiffProblem &p, const DiffGrads &g);
 int launch_diff_dlambda(const DiffProblem &p, const DiffGrads &g, int tiles, float *dlambda);
 // tensor cores: bf16, D = 64 or 128, 16-byte aligned rows (ta_diff_tc.cu)
 int launch_diff_tc(const DiffProblem &p);
+int launch_diff_tc_bwd(const DiffProblem &p, const DiffGrads &g);     // (ta_diff_tc_bwd.cu)
 
 }  // namespace ta

@@ -142,9 +142,6 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
 
-    // registers: the softmax threads hold a row of scores (384 x 168 at launch = 128 x 56 + 256 x 224)
-    if (warp < 4) {
-
     if (warp == 0) {
         // =============================================================== TMA producer
         if (lane == 0) {
@@ -262,8 +259,7 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             }
             ++ic;
         }
-    }
-    } else {
+    } else if (warp >= 4) {
         // =============================================================== softmax, epilogue
     
         const int ch = (warp - 4) >> 2, wq = warp & 3;
@@ -475,11 +471,6 @@ int launch_d(const DiffProblem &p) {
     if (!configured.is_done(dev)) {
         const cudaError_t e = cudaFuncSetAttribute(diff_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
         if (e != cudaSuccess) return cuda_fail(e);
-        // the register split must not ask for more than the block is launched with
-        cudaFuncAttributes fa;
-        const cudaError_t e2 = cudaFuncGetAttributes(&fa, diff_tc_kernel<D>);
-        if (e2 != cudaSuccess) return cuda_fail(e2);
-        if (fa.numRegs * kThreads < 128 * 56 + 256 * 224) return TA_ERR_UNSUPPORTED;
         configured.mark(dev);
     }
     const unsigned grid = (unsigned)(a.total_items < num_sms ? a.total_items : num_sms);

@@ -53,6 +53,24 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t *v) {
         : "memory");
 }
 
+// 16 columns -> registers, without the wait; registers -> 8 columns
+__device__ __forceinline__ void tmem_ld16_nowait(uint32_t taddr, uint32_t *v) {
+    __syncwarp();
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t *v) {
+    __syncwarp();
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
+
 // Zeroes rows [r0, r1) of a tile in shared memory (kSlabs slabs of 128-byte rows); the whole warp takes part.  For rows the
 // tensor holds but the call's lengths do not count: whatever stands there must not meet a weight of 0 in a product.
 __device__ __forceinline__ void zero_rows(uint32_t tile, uint32_t slab_bytes, int slabs, int r0, int r1) {

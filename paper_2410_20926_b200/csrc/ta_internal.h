@@ -221,6 +221,7 @@ int read_status_tc_backward(unsigned int *word);
 int read_status_tc_fused(unsigned int *word);
 int read_status_tc_backward_long(unsigned int *word);
 int read_status_diff_tc(unsigned int *word);
+int read_status_diff_tc_bwd(unsigned int *word);
 
 // CUDA error code seen by the last call of this host thread that returned TA_ERR_CUDA.
 extern thread_local int tl_last_cuda_error;
