@@ -14,7 +14,7 @@ OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["ta_api.cu", "ta_simt.cu", "ta_tc.cu", "ta_tc_fused.cu", "ta_tc_pair.cu", "ta_tc_long.cu", "ta_tc_bwd.cu",
            "ta_tc_bwd_long.cu", "ta_simt_bwd.cu", "ta_backward.cu", "ta_noalloc.cu", "ta_selftest.cu", "ta_pad.cu",
            "ta_rotary.cu", "ta_diff.cu", "ta_diff_simt.cu", "ta_diff_tc.cu",
-           "ta_diff_tc_bwd.cu"]
+           "ta_diff_tc_bwd.cu", "ta_diff_decode.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", HERE]
 

@@ -27,11 +27,11 @@ int check_shape(int B, int H, int H_kv, int Nq, int Nk, int D, int dtype) {
 
 bool few_rows(int H, int H_kv, int Nq) { return (long long)(H / H_kv) * Nq <= kSplitRows; }
 
-// Key ranges of the split kernels: about four blocks per SM, ranges of 256 keys or more.
+// Key ranges of the split kernels: six blocks per SM, ranges of 256 keys or more.
 int num_splits(int B, int H, int H_kv, int Nq, int Nk) {
     const long long rows = (long long)(H / H_kv) * Nq, groups = (rows + 7) / 8;
     const long long blocks = (long long)B * H_kv * groups;
-    const long long want = 4ll * current_device_sms(nullptr);
+    const long long want = 6ll * current_device_sms(nullptr);
     long long s = (want + blocks - 1) / blocks;
     const long long most = ((long long)Nk + 255) / 256;
     if (s > most) s = most;
@@ -192,12 +192,10 @@ int forward_impl(const ta_diff_params &p) {
     d.q_lens = p.q_lens; d.kv_lens = p.kv_lens;
     if (p.saved) set_saved(&d, p.saved);
     d.stream = (cudaStream_t)p.stream;
-    if (!few_rows(p.H, p.H_kv, p.Nq)) {
-        const bool tc = tc_shape(d.D, d.dtype, d.scale, p.flags) && tma_ok(d.q, d.sq, d.B, d.H, d.Nq) &&
-                        tma_ok(d.k, d.sk, d.B, d.H_kv, d.Nk) && tma_ok(d.v, d.sv, d.B, d.H_kv, d.Nk) &&
-                        tma_ok(d.out, d.so, d.B, d.H, d.Nq);
-        return tc ? launch_diff_tc(d) : launch_diff_simt(d);
-    }
+    const bool tc = tc_shape(d.D, d.dtype, d.scale, p.flags) && tma_ok(d.q, d.sq, d.B, d.H, d.Nq) &&
+                    tma_ok(d.k, d.sk, d.B, d.H_kv, d.Nk) && tma_ok(d.v, d.sv, d.B, d.H_kv, d.Nk) &&
+                    tma_ok(d.out, d.so, d.B, d.H, d.Nq);
+    if (!few_rows(p.H, p.H_kv, p.Nq)) return tc ? launch_diff_tc(d) : launch_diff_simt(d);
     char *ws = (char *)p.workspace;
     PooledGuard pooled{nullptr, d.stream};
     if (!ws) {
@@ -208,7 +206,7 @@ int forward_impl(const ta_diff_params &p) {
     part.splits = num_splits(p.B, p.H, p.H_kv, p.Nq, p.Nk);
     part.ml = (float4 *)ws;
     part.acc = (float *)(ws + up256((size_t)p.B * p.H * p.Nq * part.splits * sizeof(float4)));
-    if ((rc = launch_diff_simt_split(d, part)) != TA_OK) return rc;
+    if ((rc = tc ? launch_diff_decode(d, part) : launch_diff_simt_split(d, part)) != TA_OK) return rc;
     return launch_diff_combine(d, part);
 }
 

@@ -89,6 +89,8 @@ int launch_diff_group_sum(const DiffProblem &p, const DiffGrads &g);
 int launch_diff_dlambda(const DiffProblem &p, const DiffGrads &g, int tiles, float *dlambda);
 // tensor cores: bf16, D = 64 or 128, 16-byte aligned rows (ta_diff_tc.cu)
 int launch_diff_tc(const DiffProblem &p);
+// few query rows: bf16, D = 64 or 128, 16-byte aligned rows (ta_diff_decode.cu)
+int launch_diff_decode(const DiffProblem &p, const DiffPartials &part);
 int launch_diff_tc_bwd(const DiffProblem &p, const DiffGrads &g);     // (ta_diff_tc_bwd.cu)
 
 }  // namespace ta

@@ -391,15 +391,18 @@ diff_simt_split_kernel(const __grid_constant__ SimtArgs a) {
     }
 }
 
-// One warp per query row: joins the key ranges.  Ranges that saw nothing have m = -inf, l = 0 and sums of 0.
+// One block per query row joins its key ranges.  Ranges that saw nothing have m = -inf, l = 0 and sums of 0.  A warp's lanes
+// cover the features (float4 each where D is a multiple of 4); the warps take the ranges in turn, so that the many
+// ranges of a single long request are read at once.
+constexpr int kJoinWarps = 8;
 template <typename T>
-__global__ void __launch_bounds__(128)
+__global__ void __launch_bounds__(32 * kJoinWarps)
 diff_combine_kernel(const __grid_constant__ SimtArgs a) {
+    __shared__ float s_red[kJoinWarps][4], s_acc[kJoinWarps][2 * TA_MAX_HEAD_DIM];
     const DiffProblem &p = a.p;
     griddep_wait();
-    const long long row = blockIdx.x * 4ll + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
-    if (row >= (long long)p.B * p.H * p.Nq) return;
+    const long long row = blockIdx.x;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int t = (int)(row % p.Nq);
     const int bh = (int)(row / p.Nq), b = bh / p.H, h = bh - b * p.H;
     const int ns = a.part.splits, D = p.D;
@@ -417,24 +420,69 @@ diff_combine_kernel(const __grid_constant__ SimtArgs a) {
     }
     const bool any = m1 != -INFINITY;
     float l1 = 0.f, l2 = 0.f;
-    float acc1[8], acc2[8];
+    if (any && (D & 3) == 0) {
+        // 2 D / 4 float4 of both maps: up to 4 per lane
+        float4 acc[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) acc1[i] = acc2[i] = 0.f;
-    if (any) {
+        for (int i = 0; i < 4; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-        for (int s = 0; s < ns; ++s) {
+        for (int s = warp; s < ns; s += kJoinWarps) {
             const float4 x = ml[s];
             const float w1 = exp2f(x.x - m1), w2 = exp2f(x.z - m2);
             l1 = fmaf(x.y, w1, l1);
             l2 = fmaf(x.w, w2, l2);
-            const float *o = a.part.acc + (row * ns + s) * 2 * D;
+            const float4 *o = reinterpret_cast<const float4 *>(a.part.acc + (row * ns + s) * 2 * D);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < 4; ++i) {
                 const int c = lane + 32 * i;
-                if (c >= D) break;
-                acc1[i] = fmaf(o[c], w1, acc1[i]);
-                acc2[i] = fmaf(o[D + c], w2, acc2[i]);
+                if (4 * c >= 2 * D) break;
+                const float w = 4 * c < D ? w1 : w2;
+                const float4 y = __ldcg(o + c);
+                acc[i].x = fmaf(y.x, w, acc[i].x);
+                acc[i].y = fmaf(y.y, w, acc[i].y);
+                acc[i].z = fmaf(y.z, w, acc[i].z);
+                acc[i].w = fmaf(y.w, w, acc[i].w);
             }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = lane + 32 * i;
+            if (4 * c < 2 * D) *reinterpret_cast<float4 *>(&s_acc[warp][4 * c]) = acc[i];
+        }
+    } else {
+        for (int c = lane; c < 2 * D; c += 32) {
+            float x = 0.f;
+            for (int s = warp; any && s < ns; s += kJoinWarps)
+                x = fmaf(a.part.acc[(row * ns + s) * 2 * D + c], c < D ? exp2f(ml[s].x - m1) : exp2f(ml[s].z - m2), x);
+            s_acc[warp][c] = x;
+        }
+        for (int s = warp; any && s < ns; s += kJoinWarps) {
+            l1 = fmaf(ml[s].y, exp2f(ml[s].x - m1), l1);
+            l2 = fmaf(ml[s].w, exp2f(ml[s].z - m2), l2);
+        }
+    }
+    if (lane == 0) {
+        s_red[warp][0] = l1;
+        s_red[warp][1] = l2;
+    }
+    __syncthreads();
+    if (warp != 0) return;
+    l1 = l2 = 0.f;
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) {
+        l1 += s_red[w][0];
+        l2 += s_red[w][1];
+    }
+    float acc1[8], acc2[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        acc1[i] = acc2[i] = 0.f;
+        const int c = lane + 32 * i;
+        if (c >= D) continue;
+#pragma unroll
+        for (int w = 0; w < kJoinWarps; ++w) {
+            acc1[i] += s_acc[w][c];
+            acc2[i] += s_acc[w][D + c];
         }
     }
     const float lam = __ldg(p.lambda + (p.lambda_count > 1 ? h : 0));
@@ -454,17 +502,17 @@ diff_combine_kernel(const __grid_constant__ SimtArgs a) {
         }
         if (lane == 0) p.ostep[row] = make_float2(most1 * i1 * (1.f / 32767.f), most2 * i2 * (1.f / 32767.f));
     }
-    const float n1 = diff_inv_step(most1), n2 = diff_inv_step(most2);
+    const float n1 = any ? diff_inv_step(most1) : 0.f, n2 = any ? diff_inv_step(most2) : 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int c = lane + 32 * i;
         if (c >= D) break;
-        const float o2 = acc2[i] * i2;
-        store1(orow + c, acc1[i] * i1 - lam * o2);
+        const float o1 = any ? acc1[i] * i1 : 0.f, o2 = any ? acc2[i] * i2 : 0.f;
+        store1(orow + c, o1 - lam * o2);
         if (p.o2) p.o2[row * D + c] = o2;
         if (p.o16) {
-            p.o16[row * 2 * D + c] = (short)__float2int_rn(acc1[i] * n1);
-            p.o16[row * 2 * D + D + c] = (short)__float2int_rn(acc2[i] * n2);
+            p.o16[row * 2 * D + c] = (short)__float2int_rn(any ? acc1[i] * n1 : 0.f);
+            p.o16[row * 2 * D + D + c] = (short)__float2int_rn(any ? acc2[i] * n2 : 0.f);
         }
     }
     if (p.lse && lane == 0)
@@ -838,11 +886,11 @@ int launch_diff_combine(const DiffProblem &p, const DiffPartials &part) {
     SimtArgs a = {};
     a.p = p;
     a.part = part;
-    const long long blocks = ((long long)p.B * p.H * p.Nq + 3) / 4;
+    const long long blocks = (long long)p.B * p.H * p.Nq;
     if (blocks > 0x7FFFFFFFll) return TA_ERR_TOO_LARGE;
     if (p.dtype == TA_DTYPE_F32)
-        return launch_kernel(diff_combine_kernel<float>, (unsigned)blocks, 128, 0, p.stream, true, a);
-    return launch_kernel(diff_combine_kernel<__nv_bfloat16>, (unsigned)blocks, 128, 0, p.stream, true, a);
+        return launch_kernel(diff_combine_kernel<float>, (unsigned)blocks, 32 * kJoinWarps, 0, p.stream, true, a);
+    return launch_kernel(diff_combine_kernel<__nv_bfloat16>, (unsigned)blocks, 32 * kJoinWarps, 0, p.stream, true, a);
 }
 
 int launch_diff_stats(const DiffProblem &p, float4 *stats) {
