@@ -87,7 +87,7 @@ BackwardLayout backward_layout(int B, int H, int H_kv, int Nq, int Nk, int D, bo
     BackwardLayout L;
     const int tile = tc ? 128 : diff_simt_tile(D);
     L.hsplit = head_chunks(B, H, H_kv, Nk, tile);
-    L.dlam_parts = (Nq + tile - 1) / tile * (tc ? 8 : 1);
+    L.dlam_parts = (Nq + tile - 1) / tile * (tc ? 16 : 1);
     L.stats = 0;
     L.dlam = up256((size_t)B * H * diff_padded_rows(Nq) * sizeof(float4));
     L.part = L.dlam + up256((size_t)B * H * L.dlam_parts * sizeof(float));
@@ -251,12 +251,12 @@ int backward_impl(const ta_diff_bwd_params &p) {
         ws = (char *)pooled.ptr;
     }
     DiffGrads g = {};
-    g.stats = (const float4 *)(ws + L.stats);
+    g.stats = (const float *)(ws + L.stats);
     g.dq = p.dq; g.dk = p.dk; g.dv = p.dv;
     g.part = (float *)(ws + L.part);
     g.hsplit = L.hsplit;
     g.dlam_part = (float *)(ws + L.dlam);
-    if ((rc = launch_diff_stats(d, (float4 *)(ws + L.stats))) != TA_OK) return rc;
+    if ((rc = launch_diff_stats(d, (float *)(ws + L.stats))) != TA_OK) return rc;
     if ((rc = tc ? launch_diff_tc_bwd(d, g) : launch_diff_simt_bwd(d, g)) != TA_OK) return rc;
     if (g.hsplit > 1 && (rc = launch_diff_group_sum(d, g)) != TA_OK) return rc;
     return launch_diff_dlambda(d, g, L.dlam_parts, p.dlambda);

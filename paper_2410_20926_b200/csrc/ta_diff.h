@@ -64,17 +64,22 @@ struct DiffPartials {
     int splits;
 };
 
-// Row statistics of the backward, [B*H][rows padded to 128]: (lse_1, lse_2, d_1, d_2); rows without a visible key and
-// the padding hold (+inf, +inf, 0, 0), so that their weights come out as 0.
+// Row statistics of the backward: -lse_1, -lse_2, -d_1, -d_2 (as the kernels add them), 64 rows of each in turn, so that
+// neighbouring rows are neighbours; [B*H][rows padded to 128 / 64][4][64] floats.  Rows without a visible key and the padding
+// hold (-inf, -inf, 0, 0), so that their weights come out as 0.
 constexpr int kDiffRowPad = 128;
 inline long long diff_padded_rows(int Nq) { return ((long long)Nq + kDiffRowPad - 1) / kDiffRowPad * kDiffRowPad; }
+__device__ __forceinline__ float4 diff_row_stats(const float *stats, long long bh, long long prow, int t) {
+    const float *x = stats + (bh * prow + (t & ~63)) * 4 + (t & 63);
+    return make_float4(__ldg(x), __ldg(x + 64), __ldg(x + 128), __ldg(x + 192));
+}
 
 struct DiffGrads {
-    const float4 *stats;
+    const float *stats;
     void *dq, *dk, *dv;          // contiguous, dtype
     float *part;                 // dK, dV partials [2][hsplit][B*H_kv*Nk*D] when hsplit > 1
     int hsplit;                  // items a GQA group's query heads are split over
-    float *dlam_part;            // [B*H][parts]: sums of A_2 o dA; the tensor-core kernel writes 8 per query tile of 128, the
+    float *dlam_part;            // [B*H][parts]: sums of A_2 o dA; the tensor-core kernel writes 16 per query tile of 128, the
                                  // generic one 1 per tile
 };
 
@@ -83,7 +88,7 @@ int diff_simt_tile(int D);                       // rows of a query tile / key t
 int launch_diff_simt(const DiffProblem &p);
 int launch_diff_simt_split(const DiffProblem &p, const DiffPartials &part);
 int launch_diff_combine(const DiffProblem &p, const DiffPartials &part);
-int launch_diff_stats(const DiffProblem &p, float4 *stats);
+int launch_diff_stats(const DiffProblem &p, float *stats);
 int launch_diff_simt_bwd(const DiffProblem &p, const DiffGrads &g);
 int launch_diff_group_sum(const DiffProblem &p, const DiffGrads &g);
 int launch_diff_dlambda(const DiffProblem &p, const DiffGrads &g, int tiles, float *dlambda);

@@ -524,7 +524,7 @@ diff_combine_kernel(const __grid_constant__ SimtArgs a) {
 // One warp per row: d_c = <dout, A_c V>; in fp32 d_1 = <dout, out> + lambda d_2.
 template <typename T>
 __global__ void __launch_bounds__(128)
-diff_stats_kernel(const __grid_constant__ SimtArgs a, float4 *stats) {
+diff_stats_kernel(const __grid_constant__ SimtArgs a, float *stats) {
     const DiffProblem &p = a.p;
     const long long idx = blockIdx.x * 4ll + (threadIdx.x >> 5);
     const int lane = threadIdx.x & 31;
@@ -565,7 +565,10 @@ diff_stats_kernel(const __grid_constant__ SimtArgs a, float4 *stats) {
             d2 *= step.y;
         }
     }
-    if (lane == 0) stats[idx] = make_float4(lse.x, lse.y, d1, d2);
+    if (lane < 4) {
+        const float x = lane == 0 ? -lse.x : lane == 1 ? -lse.y : lane == 2 ? -d1 : -d2;
+        stats[((long long)bh * a.prow + (t & ~63)) * 4 + 64 * lane + (t & 63)] = x;
+    }
 }
 
 // dQ of one query tile and its share of dlambda: walks the key tiles the rows see
@@ -594,7 +597,7 @@ diff_simt_dq_kernel(const __grid_constant__ SimtArgs a) {
     for (int i = 0; i < C::kM; ++i) {
         const int t = t0 + ty + 16 * i;
         row_keys[i] = sp.keys(t, p.causal);
-        st[i] = t < p.Nq ? __ldg(a.g.stats + bh * a.prow + t) : make_float4(INFINITY, INFINITY, 0.f, 0.f);
+        st[i] = diff_row_stats(a.g.stats, bh, a.prow, t);          // (padded to whole tiles)
     }
     const float sl = p.scale * kLog2e, lam = __ldg(p.lambda + (p.lambda_count > 1 ? h : 0));
     float4 dq[C::kCh][C::kM];
@@ -623,10 +626,9 @@ diff_simt_dq_kernel(const __grid_constant__ SimtArgs a) {
 #pragma unroll
                 for (int j = 0; j < C::kM; ++j) {
                     const bool vis = u0 + tx + 16 * j < row_keys[i];
-                    const float w = vis ? exp2f(fmaf(s[i][j], sl, -(c ? st[i].y : st[i].x))) : 0.f;
+                    const float w = vis ? exp2f(fmaf(s[i][j], sl, c ? st[i].y : st[i].x)) : 0.f;
                     if (c) dlam = fmaf(w, dp[i][j], dlam);
-                    const float f = c ? -lam * p.scale : p.scale;
-                    sS[(ty + 16 * i) * C::kLp + tx + 16 * j] = w * (dp[i][j] - (c ? st[i].w : st[i].z)) * f;
+                    sS[(ty + 16 * i) * C::kLp + tx + 16 * j] = c ? w * (dp[i][j] + st[i].w) * (-lam * p.scale) : w * (dp[i][j] + st[i].z) * p.scale;
                 }
         }
         __syncthreads();
@@ -694,9 +696,7 @@ diff_simt_dkv_kernel(const __grid_constant__ SimtArgs a) {
                 __syncthreads();
                 load_tile<T, DT>(sQ, (const T *)p.q + b * p.sq.b + h * p.sq.h, p.sq.n, t0, sp.ql, p.D);
                 load_tile<T, DT>(sG, (const T *)p.dout + b * p.sdo.b + h * p.sdo.h, p.sdo.n, t0, sp.ql, p.D);
-                if (threadIdx.x < C::kRows)
-                    s_st[threadIdx.x] = t0 + (int)threadIdx.x < p.Nq ? __ldg(a.g.stats + bh * a.prow + t0 + threadIdx.x)
-                                                                    : make_float4(INFINITY, INFINITY, 0.f, 0.f);
+                if (threadIdx.x < C::kRows) s_st[threadIdx.x] = diff_row_stats(a.g.stats, bh, a.prow, t0 + (int)threadIdx.x);
                 __syncthreads();
                 float s[C::kM][C::kM], dp[C::kM][C::kM], w1[C::kM][C::kM];
                 dots<DT>(sV, sG, 0, DT, dp);                             // rows: keys, columns: query rows
@@ -711,10 +711,9 @@ diff_simt_dkv_kernel(const __grid_constant__ SimtArgs a) {
 #pragma unroll
                         for (int i = 0; i < C::kM; ++i) {
                             const bool vis = u0 + ty + 16 * i < keys;
-                            const float w = vis ? exp2f(fmaf(s[i][j], sl, -(c ? st.y : st.x))) : 0.f;
-                            const float f = c ? -lam * p.scale : p.scale;
+                            const float w = vis ? exp2f(fmaf(s[i][j], sl, c ? st.y : st.x)) : 0.f;
                             const int at = (ty + 16 * i) * C::kLp + tx + 16 * j;
-                            sS[at] = w * (dp[i][j] - (c ? st.w : st.z)) * f;
+                            sS[at] = c ? w * (dp[i][j] + st.w) * (-lam * p.scale) : w * (dp[i][j] + st.z) * p.scale;
                             if (c) sA[at] = w1[i][j] - lam * w;
                             else w1[i][j] = w;
                         }
@@ -893,7 +892,7 @@ int launch_diff_combine(const DiffProblem &p, const DiffPartials &part) {
     return launch_kernel(diff_combine_kernel<__nv_bfloat16>, (unsigned)blocks, 32 * kJoinWarps, 0, p.stream, true, a);
 }
 
-int launch_diff_stats(const DiffProblem &p, float4 *stats) {
+int launch_diff_stats(const DiffProblem &p, float *stats) {
     SimtArgs a = {};
     a.p = p;
     a.prow = diff_padded_rows(p.Nq);

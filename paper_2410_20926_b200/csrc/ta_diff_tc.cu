@@ -202,12 +202,12 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         uint32_t ic = 0, g = 0, pc = 0;              // items, key blocks, blocks of weights so far
         bool ok = true;
         auto scores = [&](int c, int qs, int st) {
-            if (lane == 0) {
+            const uint32_t ql = desc_low(sQ(qs), 16), kl = desc_low(sK(st), 16);
+            if (elect_one()) {
 #pragma unroll
                 for (int kb = 0; kb < C::kd / 16; ++kb) {
-                    const uint32_t off = map_k_off<D>(c, kb, kSlab);
-                    tc_mma_ss(tmem_base + C::kColS + c * 128, smem_desc_sw128(sQ(qs) + off, 16, 1024),
-                              smem_desc_sw128(sK(st) + off, 16, 1024), idesc_s, kb > 0);
+                    const uint32_t off = map_k_off<D>(c, kb, kSlab) >> 4;
+                    mma_ss(tmem_base + C::kColS + c * 128, ql + off, kl + off, idesc_s, kb > 0);
                 }
                 tc_commit(s_full(c));
             }
@@ -244,10 +244,13 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                     if (ok && j == 0 && ch == 0) ok = warp_wait(o_free, (ic & 1) ^ 1, 0xE15, abort_flag);
                     if (!ok) break;
                     tc_fence_after();
-                    if (lane == 0) {
-                        for (int kb = 0; kb < ksteps; ++kb)
-                            tc_mma_ts(tmem_base + C::kColO + ch * 128, tmem_base + C::kColS + ch * 128 + kb * 8,
-                                      smem_desc_sw128(sV(st) + kb * 2048, kSlab, 1024), idesc_o, (kb > 0 || j > 0) ? 1u : 0u);
+                    const uint32_t vl = desc_low(sV(st), kSlab), o = tmem_base + C::kColO + ch * 128, w = tmem_base + C::kColS + ch * 128;
+                    const uint32_t first = j > 0 ? 1u : 0u;
+                    if (elect_one()) {
+                        // (weights beyond ksteps are zeros that nothing has to multiply)
+#pragma unroll
+                        for (int kb = 0; kb < kRows / 16; ++kb)
+                            if (kb < ksteps) mma_ts(o, w + kb * 8, vl + 128u * kb, idesc_o, kb > 0 ? 1u : first);
                         if (ch == 1) tc_commit(kv_free(st));
                         if (!more) tc_commit(o_full(ch));
                         if (!more && ch == 1) tc_commit(q_free(qs));

@@ -11,16 +11,16 @@
 // bandwidth the operand reads already fill; here every sum has one place and one order, and the weights are operands
 // from tensor memory.
 //
-// Both run as two chains of 64-wide half tiles that alternate on the tensor pipe, each with a warpgroup of its own: one
-// chain's exponentials run under the other chain's products.  One CTA per SM, persistent; warp 0 loads (TMA), warp 1
-// issues the MMAs in a fixed order.  Every wait is bounded; on expiry the CTA raises a flag that ends all roles, lets
+// Both run as two chains of 64-wide half tiles that alternate on the tensor pipe, each with two warpgroups of its own that
+// take 32 columns each: one chain's exponentials run under the other chain's products, and two warps per scheduler hide
+// one another's waits.  One CTA per SM, persistent; warp 0 loads (TMA), warp 1 issues the MMAs in a fixed order.  Every wait is bounded; on expiry the CTA raises a flag that ends all roles, lets
 // its copies land, frees its tensor memory and returns.
 #include "ta_diff_tc.cuh"
 
 namespace ta {
 namespace {
 
-constexpr int kThreads = 384;
+constexpr int kThreads = 640;      // loads, MMAs, two spare warps; 16 warps on weights and dS
 constexpr int kRows = 128, kHalf = 64;
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
@@ -32,20 +32,27 @@ struct BwdArgs {
     int B, H, H_kv, g, Nq, Nk, causal;
     int tiles, tile_major;         // query tiles / key blocks per head
     int gi, hsplit;                // dK, dV: query heads per item, items per (key block, KV head)
-    long long total_items, prow;
+    int total_items;
+    long long prow;
     float scale, scale_log2;
     const int *q_lens, *kv_lens;
     const float *lambda;
     int lambda_count;
-    const float4 *stats;
+    const float *stats;
     __nv_bfloat16 *dq, *dk, *dv;
     float *part, *dlam_part;
     long long kv_elems;
 };
 
-__device__ __forceinline__ long long item_of_round(const BwdArgs &a, long long k) {
-    const long long g = gridDim.x, b = blockIdx.x;
-    const long long item = k * g + ((k & 1) ? g - 1 - b : b);
+// Where the k-step kb (16 columns of weights) of a 64-column slot stands: each half's weights over the first half of the
+// scores that the same warps have read.
+__device__ __forceinline__ constexpr uint32_t weight_col(int kb) { return (uint32_t)(kb >> 1) * 32u + (uint32_t)(kb & 1) * 8u; }
+
+// the item of a CTA's k-th round: forth and back over the CTAs, so that long and short items pair up; -1: none
+// (rounds and items fit 32 bits: launch_d sees to it)
+__device__ __forceinline__ int item_of_round(const BwdArgs &a, int k) {
+    const int g = (int)gridDim.x, b = (int)blockIdx.x;
+    const int item = k * g + ((k & 1) ? g - 1 - b : b);
     return item < a.total_items ? item : -1;
 }
 
@@ -86,19 +93,19 @@ struct DqItem {
     DiffSpan sp;
     int keys_end, nhalf;
 };
-__device__ __forceinline__ DqItem decode_dq(const BwdArgs &a, long long item) {
+__device__ __forceinline__ DqItem decode_dq(const BwdArgs &a, int item) {
     DqItem c;
-    long long bh;
-    const long long heads = (long long)a.B * a.H;
+    int bh;
+    const int heads = a.B * a.H;
     if (a.tile_major) {
-        c.tile = a.tiles - 1 - (int)(item / heads);
+        c.tile = a.tiles - 1 - item / heads;
         bh = item % heads;
     } else {
-        c.tile = a.tiles - 1 - (int)(item % a.tiles);
+        c.tile = a.tiles - 1 - item % a.tiles;
         bh = item / a.tiles;
     }
-    c.b = (int)(bh / a.H);
-    c.h = (int)(bh - (long long)c.b * a.H);
+    c.b = bh / a.H;
+    c.h = bh - c.b * a.H;
     c.hk = c.h / a.g;
     c.t0 = c.tile * kRows;
     c.sp = diff_span(a.q_lens, a.kv_lens, c.b, a.Nq, a.Nk);
@@ -130,14 +137,14 @@ diff_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
     constexpr int kB = 1 + 3 * C::kNKV;
     const uint32_t q_free = bar(kB);
     auto s_full = [&](int c) { return bar(kB + 1 + c); };      // S_1, S_2, dA of chain c complete
-    auto ds_full = [&](int c) { return bar(kB + 3 + c); };     // dS_1, dS_2 of chain c written (4 warps)
+    auto ds_full = [&](int c) { return bar(kB + 3 + c); };     // dS_1, dS_2 of chain c written (8 warps)
     const uint32_t dq_full = bar(kB + 5), dq_free = bar(kB + 6);
     uint32_t *tmem_slot = (uint32_t *)(smem + C::kOffBar + C::kNumBars * 8);
     volatile uint32_t *abort_flag = tmem_slot + 1;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
-        for (int i = 0; i < C::kNumBars; ++i) mbar_init(bar(i), i == kB + 3 || i == kB + 4 ? 4 : i == kB + 6 ? 8 : 1);
+        for (int i = 0; i < C::kNumBars; ++i) mbar_init(bar(i), i == kB + 3 || i == kB + 4 ? 8 : i == kB + 6 ? 16 : 1);
         *abort_flag = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -158,8 +165,8 @@ diff_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             uint32_t ic = 0, g = 0;
             Armed armed;
             bool ok = true;
-            for (long long round = 0; ok && round * gridDim.x < a.total_items; ++round) {
-                const long long item = item_of_round(a, round);
+            for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
+                const int item = item_of_round(a, round);
                 if (item < 0) continue;
                 const DqItem c = decode_dq(a, item);
                 if (c.nhalf == 0) continue;
@@ -196,6 +203,7 @@ diff_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         // =============================================================== MMA issuer
         constexpr uint32_t idesc_s = instr_desc(kHalf, 0);
         constexpr uint32_t idesc_q = instr_desc(C::kd, 1);
+        const uint32_t q_low = desc_low(sQ, 16), g_low = desc_low(sG, 16);
         uint32_t ic = 0, g0 = 0, sc[2] = {0, 0};     // items, key blocks before this item, half tiles of each chain
         bool ok = true;
         // S_1, S_2, dA of half tile i of the item (keys 64 i ..)
@@ -215,30 +223,29 @@ diff_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 }
             }
             tc_fence_after();
-            if (lane == 0) {
-                const uint32_t rows = (uint32_t)ch * kHalf * 128u;
-                const uint32_t col = tmem_base + ch * C::kColChain;
+            const uint32_t rows = (uint32_t)ch * kHalf * 128u;
+            const uint32_t col = tmem_base + ch * C::kColChain;
+            const uint32_t kl = desc_low(sK(st) + rows, 16), vl = desc_low(sV(st) + rows, 16);
+            if (elect_one()) {
 #pragma unroll
                 for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int kb = 0; kb < C::kd / 16; ++kb) {
-                        const uint32_t off = map_k_off<D>(m, kb, C::kSlab);
-                        tc_mma_ss(col + 64 * m, smem_desc_sw128(sQ + off, 16, 1024), smem_desc_sw128(sK(st) + rows + off, 16, 1024),
-                                  idesc_s, kb > 0);
+                        const uint32_t off = map_k_off<D>(m, kb, C::kSlab) >> 4;
+                        mma_ss(col + 64 * m, q_low + off, kl + off, idesc_s, kb > 0);
                     }
 #pragma unroll
                 for (int kb = 0; kb < D / 16; ++kb) {
-                    const uint32_t off = (kb >> 2) * C::kSlab + (kb & 3) * 32;
-                    tc_mma_ss(col + 128, smem_desc_sw128(sG + off, 16, 1024), smem_desc_sw128(sV(st) + rows + off, 16, 1024), idesc_s,
-                              kb > 0);
+                    const uint32_t off = ((kb >> 2) * C::kSlab + (kb & 3) * 32) >> 4;
+                    mma_ss(col + 128, g_low + off, vl + off, idesc_s, kb > 0);
                 }
                 tc_commit(s_full(ch));
             }
             __syncwarp();
             return true;
         };
-        for (long long round = 0; ok && round * gridDim.x < a.total_items; ++round) {
-            const long long item = item_of_round(a, round);
+        for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
+            const int item = item_of_round(a, round);
             if (item < 0) continue;
             const DqItem c = decode_dq(a, item);
             if (c.nhalf == 0) continue;
@@ -254,16 +261,16 @@ diff_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 if (ok && i == 0) ok = warp_wait(dq_free, (ic & 1) ^ 1, 0x124, abort_flag);
                 if (!ok) break;
                 tc_fence_after();
-                if (lane == 0) {
-                    const uint32_t col = tmem_base + ch * C::kColChain;
+                const uint32_t col = tmem_base + ch * C::kColChain;
+                const uint32_t kl = desc_low(sK(st) + (uint32_t)ch * kHalf * 128u, C::kSlab);
+                const uint32_t first = i > 0 ? 1u : 0u;
+                if (elect_one()) {
 #pragma unroll
                     for (int m = 0; m < 2; ++m)
 #pragma unroll
                         for (int kb = 0; kb < kHalf / 16; ++kb)
-                            tc_mma_ts(tmem_base + C::kColDQ + m * C::kd, col + 64 * m + 8 * kb,
-                                      smem_desc_sw128(sK(st) + map_n_off<D>(m, C::kSlab) + (uint32_t)(ch * kHalf + 16 * kb) * 128u,
-                                                      C::kSlab, 1024),
-                                      idesc_q, (kb > 0 || i > 0) ? 1u : 0u);
+                            mma_ts(tmem_base + C::kColDQ + m * C::kd, col + 64 * m + weight_col(kb),
+                                   kl + ((map_n_off<D>(m, C::kSlab) + 16u * kb * 128u) >> 4), idesc_q, kb > 0 ? 1u : first);
                     if (ch == 1 || i + 1 == c.nhalf) tc_commit(kv_free(st));
                     if (i + 1 == c.nhalf) {
                         tc_commit(dq_full);
@@ -278,48 +285,48 @@ diff_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         }
     } else if (warp >= 4) {
         // =============================================================== weights, dS, epilogue
-        const int ch = (warp - 4) >> 2, wq = warp & 3;
+        const int wg = (warp - 4) >> 2, ch = wg >> 1, half = wg & 1, wq = warp & 3;
         const uint32_t tmem_lane = tmem_base + ((uint32_t)(wq * 32) << 16);
-        const uint32_t col = tmem_lane + ch * C::kColChain;
+        const uint32_t col = tmem_lane + ch * C::kColChain + 32 * half;
         const int r = wq * 32 + lane;
         bool ok = true;
         uint32_t ic = 0, sc = 0;
-        for (long long round = 0; ok && round * gridDim.x < a.total_items; ++round) {
-            const long long item = item_of_round(a, round);
+        for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
+            const int item = item_of_round(a, round);
             if (item < 0) continue;
             const DqItem c = decode_dq(a, item);
             const int t = c.t0 + r;
             const int row_keys = c.sp.keys(t, a.causal);
             const long long bh = (long long)c.b * a.H + c.h;
-            const float4 st = __ldg(a.stats + bh * a.prow + t);       // (rows are padded to whole tiles)
+            const float4 st = diff_row_stats(a.stats, bh, a.prow, t);       // (rows are padded to whole tiles)
             const float2 sl2 = make_float2(a.scale_log2, a.scale_log2);
-            const float2 n1 = make_float2(-st.x, -st.x), n2 = make_float2(-st.y, -st.y);
-            const float2 d1 = make_float2(-st.z, -st.z), d2 = make_float2(-st.w, -st.w);
+            const float2 n1 = make_float2(st.x, st.x), n2 = make_float2(st.y, st.y);
+            const float2 d1 = make_float2(st.z, st.z), d2 = make_float2(st.w, st.w);
             float2 dl = make_float2(0.f, 0.f);
             for (int i = ch; i < c.nhalf; i += 2, ++sc) {
                 ok = warp_wait(s_full(ch), sc & 1, 0x130, abort_flag);
                 if (!ok) break;
                 tc_fence_after();
-                const int c_hi = row_keys - kHalf * i;
-                const bool whole = __all_sync(0xffffffffu, c_hi >= kHalf);
+                const int c_hi = row_keys - kHalf * i - 32 * half;
+                const bool whole = __all_sync(0xffffffffu, c_hi >= 32);
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
-                    uint32_t x1[32], x2[32], y[32];
-                    tmem_ld32_nowait(col + 32 * q, x1);
-                    tmem_ld32_nowait(col + 64 + 32 * q, x2);
-                    tmem_ld32_nowait(col + 128 + 32 * q, y);
+                    uint32_t x1[16], x2[16], y[16];
+                    tmem_ld16_nowait(col + 16 * q, x1);
+                    tmem_ld16_nowait(col + 64 + 16 * q, x2);
+                    tmem_ld16_nowait(col + 128 + 16 * q, y);
                     tmem_ld_wait();
                     if (!whole) {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (32 * q + e >= c_hi) {
+                        for (int e = 0; e < 16; ++e)
+                            if (16 * q + e >= c_hi) {
                                 x1[e] = x2[e] = 0xFF800000u;
                                 y[e] = 0u;
                             }
                     }
-                    uint32_t p1[16], p2[16];
+                    uint32_t p1[8], p2[8];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
+                    for (int e = 0; e < 8; ++e) {
                         float2 w1 = fma2(make_float2(__uint_as_float(x1[2 * e]), __uint_as_float(x1[2 * e + 1])), sl2, n1);
                         float2 w2 = fma2(make_float2(__uint_as_float(x2[2 * e]), __uint_as_float(x2[2 * e + 1])), sl2, n2);
                         w1.x = fast_exp2(w1.x);
@@ -333,8 +340,8 @@ diff_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                         p1[e] = pack_bf16x2(w1.x, w1.y);
                         p2[e] = pack_bf16x2(w2.x, w2.y);
                     }
-                    tmem_st16(col + 16 * q, p1);
-                    tmem_st16(col + 64 + 16 * q, p2);
+                    tmem_st8(col + 8 * q, p1);
+                    tmem_st8(col + 64 + 8 * q, p2);
                 }
                 tmem_st_wait();
                 tc_fence_before();
@@ -346,8 +353,8 @@ diff_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             float s = dl.x + dl.y;
 #pragma unroll
             for (int w = 16; w > 0; w >>= 1) s += __shfl_xor_sync(0xffffffffu, s, w);
-            if (lane == 0) a.dlam_part[(bh * a.tiles + c.tile) * 8 + (warp - 4)] = s;
-            // dQ of one map per warpgroup; -lambda and the scale are applied here, in fp32
+            if (lane == 0) a.dlam_part[(bh * a.tiles + c.tile) * 16 + (warp - 4)] = s;
+            // dQ, a quarter of the columns per warpgroup; -lambda and the scale are applied here, in fp32
             if (c.nhalf > 0) {
                 ok = warp_wait(dq_full, ic & 1, 0x131, abort_flag);
                 ++ic;
@@ -355,19 +362,20 @@ diff_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 tc_fence_after();
             }
             const float f = ch ? -a.scale * __ldg(a.lambda + (a.lambda_count > 1 ? c.h : 0)) : a.scale;
-            __nv_bfloat16 *dst = a.dq + (bh * a.Nq + t) * D + ch * C::kd;
+            __nv_bfloat16 *dst = a.dq + (bh * a.Nq + t) * D + wg * (D / 4);
 #pragma unroll 1
-            for (int i = 0; i < C::kd / 32; ++i) {
-                uint32_t v[32];
-                tmem_ld32(tmem_lane + C::kColDQ + ch * C::kd + 32 * i, v);
+            for (int i = 0; i < D / 64; ++i) {
+                uint32_t v[16];
+                tmem_ld16_nowait(tmem_lane + C::kColDQ + wg * (D / 4) + 16 * i, v);
+                tmem_ld_wait();
                 if (t >= a.Nq) continue;
 #pragma unroll
-                for (int e = 0; e < 32; e += 8) {
+                for (int e = 0; e < 16; e += 8) {
                     uint32_t w[4];
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
                         w[k] = row_keys > 0 ? pack_bf16x2(__uint_as_float(v[e + 2 * k]) * f, __uint_as_float(v[e + 2 * k + 1]) * f) : 0u;
-                    *reinterpret_cast<uint4 *>(dst + 32 * i + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                    *reinterpret_cast<uint4 *>(dst + 16 * i + e) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
             tc_fence_before();
@@ -387,7 +395,9 @@ diff_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
 // ------------------------------------------------------------------ dK, dV: one key block, all query rows that see it
 //
 // Scores transposed (rows: keys, columns: 64 query rows), so that P^T and dS^T are operands from tensor memory.  Per chain
-// two slots of 64 columns: X takes S_1, then dA, then dS_2; Y takes S_2, then P_1 - lambda P_2 and dS_1.
+// two slots of 64 columns: Y takes S_1, then P_1 - lambda P_2 and dS_1; X takes dA and, once that is in registers, S_2,
+// then dS_2.  (Every 16 columns' results go over the 16 columns of scores they come from.)  dA is the one thing a thread
+// holds: the other order, both weights held until dA comes, needs twice the registers and spills.
 
 template <int D>
 struct DkvCfg {
@@ -409,22 +419,21 @@ struct DkvItem {
     DiffSpan sp;
     int t_lo, per_head, n;        // first query row (a multiple of 64), steps per head, steps of the item
 };
-__device__ __forceinline__ DkvItem decode_dkv(const BwdArgs &a, long long item) {
+__device__ __forceinline__ DkvItem decode_dkv(const BwdArgs &a, int item) {
     DkvItem c;
     // earlier (longer, when causal) key blocks first
-    const long long per_tile = a.total_items / a.tiles;
-    int tile;
-    long long rest;
+    const int per_tile = a.total_items / a.tiles;
+    int tile, rest;
     if (a.tile_major) {
-        tile = (int)(item / per_tile);
+        tile = item / per_tile;
         rest = item % per_tile;
     } else {
-        tile = (int)(item % a.tiles);
+        tile = item % a.tiles;
         rest = item / a.tiles;
     }
-    c.hs = (int)(rest % a.hsplit); rest /= a.hsplit;
-    c.hk = (int)(rest % a.H_kv);
-    c.b = (int)(rest / a.H_kv);
+    c.hs = rest % a.hsplit; rest /= a.hsplit;
+    c.hk = rest % a.H_kv;
+    c.b = rest / a.H_kv;
     c.h0 = c.hk * a.g + c.hs * a.gi;
     c.u0 = tile * kRows;
     c.sp = diff_span(a.q_lens, a.kv_lens, c.b, a.Nq, a.Nk);
@@ -454,10 +463,10 @@ diff_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     auto q_free = [&](int i) { return bar(1 + C::kStages + i); };      // (products read it, then 4 warps its statistics)
     constexpr int kB = 1 + 2 * C::kStages;
     const uint32_t kv_free = bar(kB);
-    auto s_full = [&](int c) { return bar(kB + 1 + c); };      // S_1, S_2 of chain c complete
-    auto s_read = [&](int c) { return bar(kB + 3 + c); };      // and read into registers (4 warps)
-    auto dp_full = [&](int c) { return bar(kB + 5 + c); };     // dA of chain c complete
-    auto ds_full = [&](int c) { return bar(kB + 7 + c); };     // weights and dS of chain c written (4 warps)
+    auto s_full = [&](int c) { return bar(kB + 1 + c); };      // S_1, dA of chain c complete
+    auto da_read = [&](int c) { return bar(kB + 3 + c); };     // dA in registers (8 warps)
+    auto s2_full = [&](int c) { return bar(kB + 5 + c); };     // S_2 of chain c complete
+    auto ds_full = [&](int c) { return bar(kB + 7 + c); };     // weights and dS of chain c written (8 warps)
     const uint32_t acc_full = bar(kB + 9), acc_free = bar(kB + 10);
     uint32_t *tmem_slot = (uint32_t *)(smem + C::kOffBar + C::kNumBars * 8);
     volatile uint32_t *abort_flag = tmem_slot + 1;
@@ -466,7 +475,7 @@ diff_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     if (tid == 0) {
         for (int i = 0; i < C::kNumBars; ++i) {
             const int k = i - kB;
-            mbar_init(bar(i), k == 3 || k == 4 || k == 7 || k == 8 ? 4 : k == 10 ? 8 : 1);
+            mbar_init(bar(i), k == 3 || k == 4 || k == 7 || k == 8 ? 8 : k == 10 ? 16 : 1);
         }
         *abort_flag = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -489,8 +498,8 @@ diff_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 uint32_t ic = 0, g = 0;
                 Armed armed;
                 bool ok = true;
-                for (long long round = 0; ok && round * gridDim.x < a.total_items; ++round) {
-                    const long long item = item_of_round(a, round);
+                for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
+                    const int item = item_of_round(a, round);
                     if (item < 0) continue;
                     const DkvItem c = decode_dkv(a, item);
                     if (c.n == 0) continue;
@@ -518,7 +527,7 @@ diff_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                             tma_load_5d(sG(st) + s * C::kQSlab, &map_g, q_full(st), 64 * s, t0, 0, h, c.b);
                         }
                         // (the statistics are padded to whole tiles of rows)
-                        bulk_load(s0 + C::kOffStat + st * C::kStat, a.stats + ((long long)c.b * a.H + h) * a.prow + t0, C::kStat,
+                        bulk_load(s0 + C::kOffStat + st * C::kStat, a.stats + (((long long)c.b * a.H + h) * a.prow + t0) * 4, C::kStat,
                                   q_full(st));
                     }
                 }
@@ -529,6 +538,7 @@ diff_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             constexpr uint32_t idesc_s = instr_desc(kHalf, 0);
             constexpr uint32_t idesc_v = instr_desc(D, 1);
             constexpr uint32_t idesc_k = instr_desc(C::kd, 1);
+            const uint32_t k_low = desc_low(sK, 16), v_low = desc_low(sV, 16);
             uint32_t ic = 0, g0 = 0, sr[2] = {0, 0}, sd[2] = {0, 0};
             bool ok = true;
             auto scores = [&](const DkvItem &c, int i) {
@@ -544,20 +554,22 @@ diff_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     __syncwarp();
                 }
                 tc_fence_after();
-                if (lane == 0) {
+                const uint32_t ql = desc_low(sQ(st), 16), gl = desc_low(sG(st), 16), x = tmem_base + ch * 128, y = x + 64;
+                if (elect_one()) {
 #pragma unroll
-                    for (int m = 0; m < 2; ++m)
+                    for (int kb = 0; kb < D / 16; ++kb)
+                        mma_ss(x, v_low + (((kb >> 2) * C::kSlab + (kb & 3) * 32) >> 4),
+                               gl + (((kb >> 2) * C::kQSlab + (kb & 3) * 32) >> 4), idesc_s, kb > 0);
 #pragma unroll
-                        for (int kb = 0; kb < C::kd / 16; ++kb)
-                            tc_mma_ss(tmem_base + ch * 128 + 64 * m, smem_desc_sw128(sK + map_k_off<D>(m, kb, C::kSlab), 16, 1024),
-                                      smem_desc_sw128(sQ(st) + map_k_off<D>(m, kb, C::kQSlab), 16, 1024), idesc_s, kb > 0);
+                    for (int kb = 0; kb < C::kd / 16; ++kb)
+                        mma_ss(y, k_low + (map_k_off<D>(0, kb, C::kSlab) >> 4), ql + (map_k_off<D>(0, kb, C::kQSlab) >> 4), idesc_s, kb > 0);
                     tc_commit(s_full(ch));
                 }
                 __syncwarp();
                 return true;
             };
-            for (long long round = 0; ok && round * gridDim.x < a.total_items; ++round) {
-                const long long item = item_of_round(a, round);
+            for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
+                const int item = item_of_round(a, round);
                 if (item < 0) continue;
                 const DkvItem c = decode_dkv(a, item);
                 if (c.n == 0) continue;
@@ -566,46 +578,45 @@ diff_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 if (ok && c.n > 1) ok = scores(c, 1);
                 for (int i = 0; ok && i <= c.n; ++i) {
                     if (i < c.n) {
-                        // dA of step i, once its scores are in registers
+                        // S_2 of step i, once its dA is in registers
                         const int ch = i & 1, st = (g0 + (uint32_t)i) % C::kStages;
-                        ok = warp_wait(s_read(ch), sr[ch] & 1, 0x222, abort_flag);
+                        ok = warp_wait(da_read(ch), sr[ch] & 1, 0x222, abort_flag);
                         ++sr[ch];
                         if (!ok) break;
                         tc_fence_after();
-                        if (lane == 0) {
+                        const uint32_t ql = desc_low(sQ(st), 16), x = tmem_base + ch * 128;
+                        if (elect_one()) {
 #pragma unroll
-                            for (int kb = 0; kb < D / 16; ++kb)
-                                tc_mma_ss(tmem_base + ch * 128, smem_desc_sw128(sV + (kb >> 2) * C::kSlab + (kb & 3) * 32, 16, 1024),
-                                          smem_desc_sw128(sG(st) + (kb >> 2) * C::kQSlab + (kb & 3) * 32, 16, 1024), idesc_s, kb > 0);
-                            tc_commit(dp_full(ch));
+                            for (int kb = 0; kb < C::kd / 16; ++kb)
+                                mma_ss(x, k_low + (map_k_off<D>(1, kb, C::kSlab) >> 4), ql + (map_k_off<D>(1, kb, C::kQSlab) >> 4),
+                                       idesc_s, kb > 0);
+                            tc_commit(s2_full(ch));
                             if (i + 1 == c.n) tc_commit(kv_free);
                         }
                         __syncwarp();
                     }
                     if (i >= 1) {
-                        // dV, dK of step i - 1, then the scores of step i + 1 in the same slots
+                        // dV, dK of step i - 1, then dA and S_1 of step i + 1 in the same slots
                         const int k = i - 1, ch = k & 1, st = (g0 + (uint32_t)k) % C::kStages;
                         ok = warp_wait(ds_full(ch), sd[ch] & 1, 0x223, abort_flag);
                         ++sd[ch];
                         if (ok && k == 0) ok = warp_wait(acc_free, (ic & 1) ^ 1, 0x224, abort_flag);
                         if (!ok) break;
                         tc_fence_after();
-                        if (lane == 0) {
-                            const uint32_t x = tmem_base + ch * 128, y = x + 64;
+                        const uint32_t x = tmem_base + ch * 128, y = x + 64, first = k > 0 ? 1u : 0u;
+                        const uint32_t gl = desc_low(sG(st), C::kQSlab), ql = desc_low(sQ(st), C::kQSlab);
+                        if (elect_one()) {
 #pragma unroll
                             for (int kb = 0; kb < kHalf / 16; ++kb)
-                                tc_mma_ts(tmem_base + C::kColDV, y + 8 * kb, smem_desc_sw128(sG(st) + kb * 2048, C::kQSlab, 1024),
-                                          idesc_v, (kb > 0 || k > 0) ? 1u : 0u);
+                                mma_ts(tmem_base + C::kColDV, y + 16 * kb, gl + 128u * kb, idesc_v, kb > 0 ? 1u : first);
 #pragma unroll
                             for (int kb = 0; kb < kHalf / 16; ++kb)
-                                tc_mma_ts(tmem_base + C::kColDK, y + 32 + 8 * kb,
-                                          smem_desc_sw128(sQ(st) + map_n_off<D>(0, C::kQSlab) + kb * 2048, C::kQSlab, 1024), idesc_k,
-                                          (kb > 0 || k > 0) ? 1u : 0u);
+                                mma_ts(tmem_base + C::kColDK, y + 16 * kb + 8, ql + (map_n_off<D>(0, C::kQSlab) >> 4) + 128u * kb,
+                                       idesc_k, kb > 0 ? 1u : first);
 #pragma unroll
                             for (int kb = 0; kb < kHalf / 16; ++kb)
-                                tc_mma_ts(tmem_base + C::kColDK + C::kd, x + 8 * kb,
-                                          smem_desc_sw128(sQ(st) + map_n_off<D>(1, C::kQSlab) + kb * 2048, C::kQSlab, 1024), idesc_k,
-                                          (kb > 0 || k > 0) ? 1u : 0u);
+                                mma_ts(tmem_base + C::kColDK + C::kd, x + 16 * kb,
+                                       ql + (map_n_off<D>(1, C::kQSlab) >> 4) + 128u * kb, idesc_k, kb > 0 ? 1u : first);
                             tc_commit(q_free(st));
                             if (i == c.n) tc_commit(acc_full);
                         }
@@ -619,127 +630,153 @@ diff_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         }
     } else {
         // =============================================================== weights, dS, epilogue
-        const int ch = (warp - 4) >> 2, wq = warp & 3;
+        const int wg = (warp - 4) >> 2, ch = wg >> 1, half = wg & 1, wq = warp & 3;
         const uint32_t tmem_lane = tmem_base + ((uint32_t)(wq * 32) << 16);
-        const uint32_t x = tmem_lane + ch * 128, y = x + 64;
+        const uint32_t x = tmem_lane + ch * 128 + 32 * half, y = x + 64;
         const int r = wq * 32 + lane;
         bool ok = true;
-        uint32_t ic = 0, g0 = 0, sc = 0;
-        for (long long round = 0; ok && round * gridDim.x < a.total_items; ++round) {
-            const long long item = item_of_round(a, round);
+        uint32_t ic = 0, g = ch, sc = 0;             // g: steps of both chains, this chain's next
+        for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
+            const int item = item_of_round(a, round);
             if (item < 0) continue;
-            const DkvItem c = decode_dkv(a, item);
-            const int u = c.u0 + r;
+            // (few numbers are kept over the steps; the epilogue works the item out again)
+            int n, per_head, h, cl;                  // cl: columns of the chain's first step that do not see this key
+            {
+                const DkvItem c = decode_dkv(a, item);
+                n = c.n;
+                per_head = c.per_head;
+                h = c.h0;
+                cl = a.causal ? c.u0 + r - c.sp.off - c.t_lo - 32 * half : -0x40000000;
+            }
             const float2 sl2 = make_float2(a.scale_log2, a.scale_log2);
-            for (int i = ch; i < c.n; i += 2, ++sc) {
-                const uint32_t g = g0 + (uint32_t)i;
+            int step = ch;                           // step within the head
+            for (int i = ch; i < n; i += 2, g += 2, ++sc, step += 2) {
+                while (step >= per_head) {
+                    step -= per_head;
+                    ++h;
+                }
                 const int st = g % C::kStages;
-                const int h = c.h0 + i / c.per_head, t0 = c.t_lo + kHalf * (i % c.per_head);
-                const float4 *stat = (const float4 *)(smem + C::kOffStat + st * C::kStat);
-                const float lam = __ldg(a.lambda + (a.lambda_count > 1 ? h : 0));
-                const float2 lam2 = make_float2(lam, lam), neg = make_float2(-1.f, -1.f);
+                const float *stat = (const float *)(smem + C::kOffStat + st * C::kStat) + 32 * half;
+                const float lam = -__ldg(a.lambda + (a.lambda_count > 1 ? h : 0));
+                const float2 lam2 = make_float2(lam, lam);
                 // (its copies complete before the scores that read them)
                 ok = warp_wait(q_full(st), (g / C::kStages) & 1, 0x230, abort_flag);
                 if (ok) ok = warp_wait(s_full(ch), sc & 1, 0x231, abort_flag);
                 if (!ok) break;
                 tc_fence_after();
-                float w1[64], w2[64];
-                tmem_ld32_nowait(x, (uint32_t *)w1);
-                tmem_ld32_nowait(x + 32, (uint32_t *)w1 + 32);
-                tmem_ld32_nowait(y, (uint32_t *)w2);
-                tmem_ld32_nowait(y + 32, (uint32_t *)w2 + 32);
+                uint32_t da[32];
+                tmem_ld32_nowait(x, da);
                 tmem_ld_wait();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(s_read(ch));
+                if (lane == 0) mbar_arrive(da_read(ch));
                 // columns from c_lo on see this key (all of them below the diagonal); rows without a visible key and the
                 // padding have a log-sum-exp of +inf, which makes their weights 0
-                const int c_lo = a.causal ? u - c.sp.off - t0 : 0;
+                const int c_lo = cl - kHalf * step;
                 const bool whole = __all_sync(0xffffffffu, c_lo <= 0);
-                if (!whole) {
-#pragma unroll
-                    for (int e = 0; e < 64; ++e)
-                        if (e < c_lo) w1[e] = w2[e] = -INFINITY;
-                }
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
-                    uint32_t pk[16];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        // (keeps the statistics' loads near their use: all of them at once would spill)
-                        if (e % 4 == 0) asm volatile("" ::: "memory");
-                        const int k = 32 * q + 2 * e;
-                        const float4 sa = stat[k], sb = stat[k + 1];
-                        float2 p1 = fma2(make_float2(w1[k], w1[k + 1]), sl2, make_float2(-sa.x, -sb.x));
-                        float2 p2 = fma2(make_float2(w2[k], w2[k + 1]), sl2, make_float2(-sa.y, -sb.y));
-                        p1.x = fast_exp2(p1.x);
-                        p1.y = fast_exp2(p1.y);
-                        p2.x = fast_exp2(p2.x);
-                        p2.y = fast_exp2(p2.y);
-                        p2 = mul2(p2, lam2);                           // from here on lambda P_2
-                        w1[k] = p1.x; w1[k + 1] = p1.y;
-                        w2[k] = p2.x; w2[k + 1] = p2.y;
-                        const float2 d = fma2(p2, neg, p1);
-                        pk[e] = pack_bf16x2(d.x, d.y);
-                    }
-                    tmem_st16(y + 16 * q, pk);
-                }
-                ok = warp_wait(dp_full(ch), sc & 1, 0x232, abort_flag);
-                if (!ok) break;
-                tc_fence_after();
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    uint32_t v[16], p1[8], p2[8];
-                    tmem_ld16_nowait(x + 16 * q, v);
+                    uint32_t s1[16];
+                    tmem_ld16_nowait(y + 16 * q, s1);
                     tmem_ld_wait();
+                    if (!whole) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        if (e % 4 == 0) asm volatile("" ::: "memory");
-                        const int k = 16 * q + 2 * e;
-                        const float2 sa = *(const float2 *)&stat[k].z, sb = *(const float2 *)&stat[k + 1].z;
-                        const float2 da = make_float2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
-                        const float2 s1 = mul2(make_float2(w1[k], w1[k + 1]), add2(da, make_float2(-sa.x, -sb.x)));
-                        const float2 s2 = mul2(make_float2(w2[k], w2[k + 1]), fma2(da, neg, make_float2(sa.y, sb.y)));
-                        p1[e] = pack_bf16x2(s1.x, s1.y);
-                        p2[e] = pack_bf16x2(s2.x, s2.y);
+                        for (int e = 0; e < 16; ++e)
+                            if (16 * q + e < c_lo) s1[e] = 0xFF800000u;
                     }
-                    tmem_st8(y + 32 + 8 * q, p1);
-                    tmem_st8(x + 8 * q, p2);                           // (columns of dA already read)
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        const float4 l1 = *(const float4 *)(stat + 16 * q + e);
+                        const float2 pa = fma2(make_float2(__uint_as_float(s1[e]), __uint_as_float(s1[e + 1])), sl2, make_float2(l1.x, l1.y));
+                        const float2 pb = fma2(make_float2(__uint_as_float(s1[e + 2]), __uint_as_float(s1[e + 3])), sl2, make_float2(l1.z, l1.w));
+                        s1[e] = __float_as_uint(fast_exp2(pa.x));
+                        s1[e + 1] = __float_as_uint(fast_exp2(pa.y));
+                        s1[e + 2] = __float_as_uint(fast_exp2(pb.x));
+                        s1[e + 3] = __float_as_uint(fast_exp2(pb.y));
+                    }
+                    if (q == 0) {
+                        ok = warp_wait(s2_full(ch), sc & 1, 0x232, abort_flag);
+                        if (!ok) break;
+                        tc_fence_after();
+                    }
+#pragma unroll
+                    for (int z = 0; z < 2; ++z) {
+                        uint32_t s2[8], w[4], g1[4], g2[4];
+                        tmem_ld8_nowait(x + 16 * q + 8 * z, s2);
+                        tmem_ld_wait();
+                        if (!whole) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (16 * q + 8 * z + e < c_lo) s2[e] = 0xFF800000u;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; e += 4) {
+                            const int k = 16 * q + 8 * z + e;
+                            const float4 l2 = *(const float4 *)(stat + 64 + k);
+                            const float4 d1 = *(const float4 *)(stat + 128 + k), d2 = *(const float4 *)(stat + 192 + k);
+#pragma unroll
+                            for (int f = 0; f < 2; ++f) {
+                                const int j = e + 2 * f;
+                                const float2 p1 = make_float2(__uint_as_float(s1[8 * z + j]), __uint_as_float(s1[8 * z + j + 1]));
+                                float2 p2 = fma2(make_float2(__uint_as_float(s2[j]), __uint_as_float(s2[j + 1])), sl2,
+                                                 f ? make_float2(l2.z, l2.w) : make_float2(l2.x, l2.y));
+                                p2.x = fast_exp2(p2.x);
+                                p2.y = fast_exp2(p2.y);
+                                p2 = mul2(p2, lam2);                   // -lambda P_2
+                                const float2 v = make_float2(__uint_as_float(da[k + 2 * f]), __uint_as_float(da[k + 2 * f + 1]));
+                                const float2 x1 = mul2(p1, add2(v, f ? make_float2(d1.z, d1.w) : make_float2(d1.x, d1.y)));
+                                const float2 x2 = mul2(p2, add2(v, f ? make_float2(d2.z, d2.w) : make_float2(d2.x, d2.y)));
+                                const float2 d = add2(p1, p2);
+                                w[j / 2] = pack_bf16x2(d.x, d.y);
+                                g1[j / 2] = pack_bf16x2(x1.x, x1.y);
+                                g2[j / 2] = pack_bf16x2(x2.x, x2.y);
+                            }
+                        }
+                        tmem_st4(y + 16 * q + 4 * z, w);
+                        tmem_st4(y + 16 * q + 8 + 4 * z, g1);
+                        tmem_st4(x + 16 * q + 4 * z, g2);
+                    }
                 }
+                if (!ok) break;
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(ds_full(ch));
             }
             if (!ok) break;
-            g0 += (uint32_t)c.n;
+            // the item's steps, of which this chain has taken its own: on to the chain's first of the next item
+            g += (uint32_t)(n - (n - ch + 1) / 2 * 2);
+            const DkvItem c = decode_dkv(a, item);
+            const int u = c.u0 + r;
             if (c.n > 0) {
                 ok = warp_wait(acc_full, ic & 1, 0x233, abort_flag);
                 ++ic;
                 if (!ok) break;
                 tc_fence_after();
             }
-            // warpgroup 0 writes dK (scaled), warpgroup 1 dV
+            // warpgroups 0, 1 write the halves of dK (scaled), 2, 3 those of dV
             const bool in = u < a.Nk, any = c.n > 0 && u < c.sp.kl;
             const float f = ch ? 1.f : a.scale;
-            const long long row = (((long long)c.b * a.H_kv + c.hk) * a.Nk + u) * D;
+            const int col0 = half * (D / 2);
+            const long long row = (((long long)c.b * a.H_kv + c.hk) * a.Nk + u) * D + col0;
 #pragma unroll 1
             for (int i = 0; i < D / 32; ++i) {
-                uint32_t v[32];
-                tmem_ld32(tmem_lane + (ch ? C::kColDV : C::kColDK) + 32 * i, v);
+                uint32_t v[16];
+                tmem_ld16_nowait(tmem_lane + (ch ? C::kColDV : C::kColDK) + col0 + 16 * i, v);
+                tmem_ld_wait();
                 if (!in) continue;
                 if (a.hsplit > 1) {
-                    float *dst = a.part + (ch * a.hsplit + c.hs) * a.kv_elems + row + 32 * i;
+                    float *dst = a.part + (ch * a.hsplit + c.hs) * a.kv_elems + row + 16 * i;
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4)
+                    for (int e = 0; e < 16; e += 4)
                         *reinterpret_cast<float4 *>(dst + e) =
                             any ? make_float4(__uint_as_float(v[e]) * f, __uint_as_float(v[e + 1]) * f, __uint_as_float(v[e + 2]) * f,
                                               __uint_as_float(v[e + 3]) * f)
                                 : make_float4(0.f, 0.f, 0.f, 0.f);
                 } else {
-                    __nv_bfloat16 *dst = (ch ? a.dv : a.dk) + row + 32 * i;
+                    __nv_bfloat16 *dst = (ch ? a.dv : a.dk) + row + 16 * i;
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8) {
+                    for (int e = 0; e < 16; e += 8) {
                         uint32_t w[4];
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
@@ -797,13 +834,16 @@ int launch_d(const DiffProblem &p, const DiffGrads &g) {
     a.gi = a.g / g.hsplit;
 
     a.tiles = (p.Nq + kRows - 1) / kRows;
-    a.total_items = (long long)p.B * p.H * a.tiles;
+    const long long dq_items = (long long)p.B * p.H * a.tiles;
+    const long long dkv_items = (long long)p.B * p.H_kv * g.hsplit * ((p.Nk + kRows - 1) / kRows);
+    if (dq_items > 0x3FFFFFFFll || dkv_items > 0x3FFFFFFFll) return TA_ERR_TOO_LARGE;
+    a.total_items = (int)dq_items;
     a.tile_major = 2ull * p.B * p.H_kv * p.Nk * D * 2 <= (96ull << 20) ? 1 : 0;
     rc = launch_kernel(diff_tc_dq_kernel<D>, (unsigned)(a.total_items < num_sms ? a.total_items : num_sms), kThreads,
                        DqCfg<D>::kSmem, p.stream, false, mq, mg, mk, mv, a);
     if (rc != TA_OK) return rc;
     a.tiles = (p.Nk + kRows - 1) / kRows;
-    a.total_items = (long long)p.B * p.H_kv * g.hsplit * a.tiles;
+    a.total_items = (int)dkv_items;
     a.tile_major = 2ull * p.B * p.H * p.Nq * D * 2 <= (96ull << 20) ? 1 : 0;
     return launch_kernel(diff_tc_dkv_kernel<D>, (unsigned)(a.total_items < num_sms ? a.total_items : num_sms), kThreads,
                          DkvCfg<D>::kSmem, p.stream, false, mqh, mgh, mk, mv, a);
