@@ -521,23 +521,39 @@ diff_combine_kernel(const __grid_constant__ SimtArgs a) {
 
 // ------------------------------------------------------------------ backward
 
-// One warp per row: d_c = <dout, A_c V>; in fp32 d_1 = <dout, out> + lambda d_2.
-template <typename T>
+// d_c = <dout, A_c V> row by row (in fp32 d_1 = <dout, out> + lambda d_2): a group of lanes per row that reads 16 bytes of
+// dout per lane where its rows allow (kV = 8; 32 lanes and single elements otherwise).  Bound by memory.
+template <typename T, int kV>
 __global__ void __launch_bounds__(128)
 diff_stats_kernel(const __grid_constant__ SimtArgs a, float *stats) {
     const DiffProblem &p = a.p;
-    const long long idx = blockIdx.x * 4ll + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
+    const int lanes = kV > 1 ? p.D / kV : 32;              // per row: 8 or 16
+    const long long idx = (blockIdx.x * 128ll + threadIdx.x) / lanes;
+    const int lane = threadIdx.x % lanes;
     const int bh = (int)(idx / a.prow), t = (int)(idx - bh * a.prow);
-    if (bh >= p.B * p.H) return;
+    const bool in = bh < p.B * p.H;
     const int b = bh / p.H, h = bh - b * p.H;
     const long long row = (long long)bh * p.Nq + t;
     float2 lse = make_float2(INFINITY, INFINITY);
     float d1 = 0.f, d2 = 0.f;
-    if (t < p.Nq) lse = p.lse[row];
-    if (lse.x < INFINITY) {
+    if (in && t < p.Nq) lse = p.lse[row];
+    const bool any = lse.x < INFINITY;
+    if (any) {
         const T *g = (const T *)p.dout + b * p.sdo.b + h * p.sdo.h + (long long)t * p.sdo.n;
-        if constexpr (sizeof(T) == 4) {
+        if constexpr (kV > 1) {
+            const uint4 x = __ldg(reinterpret_cast<const uint4 *>(g + kV * lane));
+            const short *o = p.o16 + row * 2 * p.D + kV * lane;
+            const uint4 y = __ldg(reinterpret_cast<const uint4 *>(o)), z = __ldg(reinterpret_cast<const uint4 *>(o + p.D));
+            const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w}, zs[4] = {z.x, z.y, z.z, z.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float lo = __uint_as_float(xs[i] << 16), hi = __uint_as_float(xs[i] & 0xFFFF0000u);
+                d1 = fmaf(lo, (float)(short)(ys[i] & 0xFFFFu), d1);
+                d1 = fmaf(hi, (float)((int)ys[i] >> 16), d1);
+                d2 = fmaf(lo, (float)(short)(zs[i] & 0xFFFFu), d2);
+                d2 = fmaf(hi, (float)((int)zs[i] >> 16), d2);
+            }
+        } else if constexpr (sizeof(T) == 4) {
             const T *o = (const T *)p.out + b * p.so.b + h * p.so.h + (long long)t * p.so.n;
             for (int c = lane; c < p.D; c += 32) {
                 const float x = load1(g + c);
@@ -552,11 +568,12 @@ diff_stats_kernel(const __grid_constant__ SimtArgs a, float *stats) {
                 d2 = fmaf(x, (float)o[p.D + c], d2);
             }
         }
-#pragma unroll
-        for (int w = 16; w > 0; w >>= 1) {
-            d1 += __shfl_xor_sync(0xffffffffu, d1, w);
-            d2 += __shfl_xor_sync(0xffffffffu, d2, w);
-        }
+    }
+    for (int w = lanes / 2; w > 0; w >>= 1) {
+        d1 += __shfl_xor_sync(0xffffffffu, d1, w);
+        d2 += __shfl_xor_sync(0xffffffffu, d2, w);
+    }
+    if (any) {
         if constexpr (sizeof(T) == 4) {
             d1 = fmaf(__ldg(p.lambda + (p.lambda_count > 1 ? h : 0)), d2, d1);
         } else {
@@ -565,7 +582,7 @@ diff_stats_kernel(const __grid_constant__ SimtArgs a, float *stats) {
             d2 *= step.y;
         }
     }
-    if (lane < 4) {
+    if (in && lane < 4) {
         const float x = lane == 0 ? -lse.x : lane == 1 ? -lse.y : lane == 2 ? -d1 : -d2;
         stats[((long long)bh * a.prow + (t & ~63)) * 4 + 64 * lane + (t & 63)] = x;
     }
@@ -896,11 +913,16 @@ int launch_diff_stats(const DiffProblem &p, float *stats) {
     SimtArgs a = {};
     a.p = p;
     a.prow = diff_padded_rows(p.Nq);
-    const long long blocks = ((long long)p.B * p.H * a.prow + 3) / 4;
+    const long long rows = (long long)p.B * p.H * a.prow;
+    // 16-byte pieces of dout: a power of two of lanes per row, rows on 16-byte boundaries
+    const bool wide = p.dtype == TA_DTYPE_BF16 && (p.D == 64 || p.D == 128) && (uintptr_t)p.dout % 16 == 0 && p.sdo.b % 8 == 0 &&
+                      p.sdo.h % 8 == 0 && p.sdo.n % 8 == 0;
+    const long long blocks = (rows * (wide ? p.D / 8 : 32) + 127) / 128;
     if (blocks > 0x7FFFFFFFll) return TA_ERR_TOO_LARGE;
     if (p.dtype == TA_DTYPE_F32)
-        return launch_kernel(diff_stats_kernel<float>, (unsigned)blocks, 128, 0, p.stream, false, a, stats);
-    return launch_kernel(diff_stats_kernel<__nv_bfloat16>, (unsigned)blocks, 128, 0, p.stream, false, a, stats);
+        return launch_kernel(diff_stats_kernel<float, 1>, (unsigned)blocks, 128, 0, p.stream, false, a, stats);
+    if (wide) return launch_kernel(diff_stats_kernel<__nv_bfloat16, 8>, (unsigned)blocks, 128, 0, p.stream, false, a, stats);
+    return launch_kernel(diff_stats_kernel<__nv_bfloat16, 1>, (unsigned)blocks, 128, 0, p.stream, false, a, stats);
 }
 
 int launch_diff_simt_bwd(const DiffProblem &p, const DiffGrads &g) {

@@ -2,51 +2,56 @@
 //
 //     out = (A_1 - lambda A_2) V,   A_c = softmax(Q_c K_c^T scale o M)
 //
-// A work item is one tile of 128 query rows of one head.  Its keys go by once in blocks of 128; the two maps are two
-// chains that share the K and V blocks and alternate on the tensor pipe.  Per chain c and key block j
+// A work item is one tile of 128 query rows of one head.  Its keys go by once in half blocks of 64; the two maps are two
+// chains that share the K and V they load.  Per chain c and half block h
 //     S_c = Q_c K_c^T                      (half the head dim, fp32 in tensor memory)
 //     m <- max(m, rowmax),  P = 2^(S scale log2 e - m) -> bf16, over S in tensor memory,  l <- l alpha + rowsum P
 //     O_c <- alpha O_c + P V               (whole head dim)
 // and at the end out = O_1 / l_1 - lambda O_2 / l_2: the sums l_c are known only then, so the maps cannot be subtracted
 // before the value product, and the pass needs 6 D multiply-adds per visible pair where the definition has 4 D.
-// S_1, S_2, O_1, O_2 fill the tensor memory (4 x 128 columns).
+// Tensor memory: two score slots of 64 columns per chain, so that a chain's next scores are formed while it works on
+// these, and O_1, O_2 -- 512 columns at head dim 128.
 //
-// One CTA per SM, persistent: warp 0 loads (TMA), warp 1 issues the MMAs in a fixed order -- P V of block j, then S of
-// block j + 1, chain after chain, so that one chain's exponentials run under the other chain's products --, warps 4-7 and
-// 8-11 are the softmax of chain 1 and 2 (one query row per thread, its 128 scores in registers).  A running maximum
-// is moved (and O rescaled) only when it has grown by more than 2^8: weights up to 256 lose nothing in bf16 or fp32.
-// Every wait is bounded; when one expires the CTA raises a flag that ends all roles, lets its copies land, frees its
-// tensor memory and returns.
+// One CTA per SM, persistent: warp 0 loads (TMA), warp 1 issues the MMAs in a fixed order -- P V of half block h, then S of
+// half block h + 2 into the slot this frees, chain after chain --, warps 4-7 and 8-11 are the softmax of chain 1 and 2
+// (one query row per thread).  A quarter of the exponentials are polynomials on the multiply-add pipes (exp2_poly).  A
+// running maximum is moved (and O rescaled) only when it has grown by more than 2^8: weights up to 256 lose nothing in
+// bf16 or fp32.  Every wait is bounded; when one expires the CTA raises a flag that ends all roles, lets its copies land,
+// frees its tensor memory and returns.
+//
+// Per 128 x 128 pairs of rows and keys and both maps, in cycles: MMAs 1792 (a 128 x 64 product from shared memory takes 48
+// where the pipe would need 32: reading its operands bounds it), exponentials 2048 on the special-function unit alone,
+// 1536 so.
 #include "ta_diff_tc.cuh"
 
 namespace ta {
 namespace {
 
-constexpr int kRows = 128;
+constexpr int kRows = 128, kHalf = 64;
 constexpr int kThreads = 384;
-constexpr uint32_t kSlab = kRows * 128;
+constexpr uint32_t kSlab = kRows * 128, kHSlab = kHalf * 128;
 
 template <int D>
 struct Cfg {
     static constexpr int kSlabs = D / 64;
     static constexpr int kd = D / 2;
-    static constexpr uint32_t kTile = kSlabs * kSlab;
+    static constexpr uint32_t kTile = kSlabs * kSlab, kHTile = kSlabs * kHSlab;
     static constexpr int kNQ = 2;
-    static constexpr int kNKV = D == 128 ? 2 : 4;
+    static constexpr int kNKV = 5;                 // stages of 64 keys, K and V apart
     static constexpr uint32_t kOffQ = 0;
     static constexpr uint32_t kOffK = kOffQ + kNQ * kTile;
-    static constexpr uint32_t kOffV = kOffK + kNKV * kTile;
-    static constexpr uint32_t kOffBar = kOffV + kNKV * kTile;
-    static constexpr int kNumBars = 2 * kNQ + 3 * kNKV + 2 + 2 + 2 + 2;
+    static constexpr uint32_t kOffV = kOffK + kNKV * kHTile;
+    static constexpr uint32_t kOffBar = kOffV + kNKV * kHTile;
+    static constexpr int kNumBars = 2 * kNQ + 4 * kNKV + 4 + 4 + 2 + 2 + 2;
     static constexpr uint32_t kOffX = kOffBar + ((kNumBars * 8 + 16 + 15) & ~15);      // 1 / l of both maps, 128 rows
     static constexpr uint32_t kSmem = kOffX + 2 * kRows * 4 + 1024;
-    static constexpr uint32_t kColS = 0, kColO = 256;
+    static constexpr uint32_t kColO = 256;
 };
 
 struct TcArgs {
     int B, H, H_kv, g, Nq, Nk, causal;
     int qtiles, tile_major;
-    long long total_items;
+    int total_items;
     float scale_log2;
     const int *q_lens, *kv_lens;
     const float *lambda;
@@ -61,40 +66,32 @@ struct TcArgs {
 struct Item {
     int b, h, hk, t0;
     DiffSpan sp;
-    int keys_end, nblocks;       // keys any row of the tile sees
+    int keys_end, n;             // keys any row of the tile sees, half blocks of them
 };
-__device__ __forceinline__ Item decode(const TcArgs &a, long long item) {
+__device__ __forceinline__ Item decode(const TcArgs &a, int item) {
     Item c;
-    int tile;
-    long long bh;
-    const long long heads = (long long)a.B * a.H;
+    int tile, bh;
+    const int heads = a.B * a.H;
     // Later (longer, when causal) tiles first.  While all K and V fit the L2 the tile is the slowest index, so the
     // numbering runs from the longest items to the shortest over the whole launch; beyond that the tiles of a head
     // stay together.
     if (a.tile_major) {
-        tile = a.qtiles - 1 - (int)(item / heads);
+        tile = a.qtiles - 1 - item / heads;
         bh = item % heads;
     } else {
-        tile = a.qtiles - 1 - (int)(item % a.qtiles);
+        tile = a.qtiles - 1 - item % a.qtiles;
         bh = item / a.qtiles;
     }
-    c.b = (int)(bh / a.H);
-    c.h = (int)(bh - (long long)c.b * a.H);
+    c.b = bh / a.H;
+    c.h = bh - c.b * a.H;
     c.hk = c.h / a.g;
     c.t0 = tile * kRows;
     c.sp = diff_span(a.q_lens, a.kv_lens, c.b, a.Nq, a.Nk);
     const int last = min(c.t0 + kRows, c.sp.ql) - 1;      // the last valid row sees the most
     c.keys_end = last >= c.t0 ? c.sp.keys(last, a.causal) : 0;
-    c.nblocks = (c.keys_end + kRows - 1) / kRows;
+    c.n = (c.keys_end + kHalf - 1) / kHalf;
     return c;
 }
-// the item of a CTA's k-th round: forth and back over the CTAs, so that long and short items pair up
-__device__ __forceinline__ long long item_of_round(const TcArgs &a, long long k) {
-    const long long g = gridDim.x, b = blockIdx.x;
-    const long long item = k * g + ((k & 1) ? g - 1 - b : b);
-    return item < a.total_items ? item : -1;
-}
-
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
@@ -104,21 +101,25 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     const uint32_t s0 = smem_u32(smem);
     auto sQ = [&](int i) { return s0 + C::kOffQ + (uint32_t)i * C::kTile; };
-    auto sK = [&](int i) { return s0 + C::kOffK + (uint32_t)i * C::kTile; };
-    auto sV = [&](int i) { return s0 + C::kOffV + (uint32_t)i * C::kTile; };
+    auto sK = [&](int i) { return s0 + C::kOffK + (uint32_t)i * C::kHTile; };
+    auto sV = [&](int i) { return s0 + C::kOffV + (uint32_t)i * C::kHTile; };
     const uint32_t bar0 = s0 + C::kOffBar;
     auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
+    // barriers 0 .. kNQ + 2 kNKV - 1 are those copies complete on
     auto q_full = [&](int i) { return bar(i); };
-    auto q_free = [&](int i) { return bar(C::kNQ + i); };
-    auto k_full = [&](int i) { return bar(2 * C::kNQ + i); };
-    auto v_full = [&](int i) { return bar(2 * C::kNQ + C::kNKV + i); };
-    auto kv_free = [&](int i) { return bar(2 * C::kNQ + 2 * C::kNKV + i); };
-    constexpr int kB = 2 * C::kNQ + 3 * C::kNKV;
-    auto s_full = [&](int c) { return bar(kB + c); };          // scores of chain c complete
-    auto p_full = [&](int c) { return bar(kB + 2 + c); };      // weights of chain c written (4 warps)
-    auto o_full = [&](int c) { return bar(kB + 4 + c); };      // value sum of chain c complete
-    const uint32_t o_free = bar(kB + 6);                       // both value sums read (8 warps)
-    const uint32_t x_full = bar(kB + 7);                       // 1 / l of both maps written (8 warps)
+    auto k_full = [&](int i) { return bar(C::kNQ + i); };
+    auto v_full = [&](int i) { return bar(C::kNQ + C::kNKV + i); };
+    constexpr int kA = C::kNQ + 2 * C::kNKV;
+    auto q_free = [&](int i) { return bar(kA + i); };
+    auto k_free = [&](int i) { return bar(kA + C::kNQ + i); };
+    auto v_free = [&](int i) { return bar(kA + C::kNQ + C::kNKV + i); };
+    constexpr int kB = 2 * C::kNQ + 4 * C::kNKV;
+    auto s_full = [&](int c, int p) { return bar(kB + 2 * c + p); };       // scores of chain c in slot p complete
+    auto p_full = [&](int c, int p) { return bar(kB + 4 + 2 * c + p); };   // weights of chain c in slot p written (4 warps)
+    auto pv_done = [&](int c) { return bar(kB + 8 + c); };                 // a value product of chain c complete
+    auto o_full = [&](int c) { return bar(kB + 10 + c); };                 // value sum of chain c complete
+    const uint32_t o_free = bar(kB + 12);                                  // both value sums read (8 warps)
+    const uint32_t x_full = bar(kB + 13);                                  // 1 / l of both maps written (8 warps)
     uint32_t *tmem_slot = (uint32_t *)(smem + C::kOffBar + C::kNumBars * 8);
     volatile uint32_t *abort_flag = tmem_slot + 1;
     float *s_inv = (float *)(smem + C::kOffX);
@@ -127,7 +128,7 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     // rows a tensor does not have arrive as zeros (TMA fill); nothing reads shared memory before it is loaded
     if (tid == 0) {
         for (int i = 0; i < C::kNumBars; ++i)
-            mbar_init(bar(i), i == kB + 2 || i == kB + 3 ? 4 : i >= kB + 6 ? 8 : 1);
+            mbar_init(bar(i), i >= kB + 4 && i < kB + 8 ? 4 : i >= kB + 12 ? 8 : 1);
         *abort_flag = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -144,178 +145,167 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 
     if (warp == 0) {
         // =============================================================== TMA producer
-        if (lane == 0) {
-            uint32_t ic = 0, g = 0;
-            uint32_t armed = 0, last_par = 0;        // bits: q, k, v slots
-            auto arm = [&](int slot, uint32_t parity) {
-                const uint32_t bit = 1u << slot;
-                armed |= bit;
-                last_par = parity ? (last_par | bit) : (last_par & ~bit);
-            };
+        if (elect_one()) {
+            Ring<C::kNQ> q;
+            Ring<C::kNKV> kv;
+            Armed armed;
             bool ok = true;
-            for (long long round = 0; ok && round * gridDim.x < a.total_items; ++round) {
-                const long long item = item_of_round(a, round);
+            for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
+                const int item = item_of_round(a.total_items, round);
                 if (item < 0) continue;
                 const Item c = decode(a, item);
-                if (c.nblocks == 0) continue;
-                const int qs = ic % C::kNQ;
-                const uint32_t qp = (ic / C::kNQ) & 1;
-                ++ic;
-                ok = mbar_wait_abortable(q_free(qs), qp ^ 1, 0xD10, abort_flag);
+                if (c.n == 0) continue;
+                ok = mbar_wait_abortable(q_free(q.st), q.ph ^ 1, 0xD10, abort_flag);
                 if (!ok) break;
-                mbar_expect_tx(q_full(qs), C::kTile);
-                arm(qs, qp);
-#pragma unroll
-                for (int s = 0; s < C::kSlabs; ++s)
-                    tma_load_5d(sQ(qs) + s * kSlab, &map_q, q_full(qs), 64 * s, c.t0, 0, c.h, c.b);
-                for (int j = 0; j < c.nblocks; ++j, ++g) {
-                    const int st = g % C::kNKV;
-                    const uint32_t par = (g / C::kNKV) & 1;
-                    ok = mbar_wait_abortable(kv_free(st), par ^ 1, 0xD11, abort_flag);
+                mbar_expect_tx(q_full(q.st), C::kTile);
+                armed.arm(q.st, q.ph);
+                tma_load_5d(sQ(q.st), &map_q, q_full(q.st), 0, c.t0, 0, c.h, c.b);
+                q.next();
+                for (int j = 0; j < c.n; ++j, kv.next()) {
+                    ok = mbar_wait_abortable(k_free(kv.st), kv.ph ^ 1, 0xD11, abort_flag);
                     if (!ok) break;
-                    mbar_expect_tx(k_full(st), C::kTile);
-                    arm(C::kNQ + st, par);
-#pragma unroll
-                    for (int s = 0; s < C::kSlabs; ++s)
-                        tma_load_5d(sK(st) + s * kSlab, &map_k, k_full(st), 64 * s, kRows * j, 0, c.hk, c.b);
-                    mbar_expect_tx(v_full(st), C::kTile);
-                    arm(C::kNQ + C::kNKV + st, par);
-#pragma unroll
-                    for (int s = 0; s < C::kSlabs; ++s)
-                        tma_load_5d(sV(st) + s * kSlab, &map_v, v_full(st), 64 * s, kRows * j, 0, c.hk, c.b);
+                    mbar_expect_tx(k_full(kv.st), C::kHTile);
+                    armed.arm(C::kNQ + kv.st, kv.ph);
+                    tma_load_5d(sK(kv.st), &map_k, k_full(kv.st), 0, kHalf * j, 0, c.hk, c.b);
+                    ok = mbar_wait_abortable(v_free(kv.st), kv.ph ^ 1, 0xD12, abort_flag);
+                    if (!ok) break;
+                    mbar_expect_tx(v_full(kv.st), C::kHTile);
+                    armed.arm(C::kNQ + C::kNKV + kv.st, kv.ph);
+                    tma_load_5d(sV(kv.st), &map_v, v_full(kv.st), 0, kHalf * j, 0, c.hk, c.b);
                 }
             }
-            if (!ok) {
-                const unsigned long long t0 = globaltimer_ns();
-                for (int slot = 0; slot < C::kNQ + 2 * C::kNKV; ++slot) {
-                    if (!(armed & (1u << slot))) continue;
-                    const uint32_t b = slot < C::kNQ ? q_full(slot) : bar(2 * C::kNQ + slot - C::kNQ);
-                    while (!mbar_try_wait(b, (last_par >> slot) & 1u) && globaltimer_ns() - t0 < 10000000ull) {
-                    }
-                }
-            }
+            if (!ok) armed.drain(bar0, kA);
         }
     } else if (warp == 1) {
-        // =============================================================== MMA issuer (lane 0 issues, the warp waits)
-        constexpr uint32_t idesc_s = instr_desc(128, 0);
-        constexpr uint32_t idesc_o = instr_desc(D, 1);
-        uint32_t ic = 0, g = 0, pc = 0;              // items, key blocks, blocks of weights so far
-        bool ok = true;
-        auto scores = [&](int c, int qs, int st) {
-            const uint32_t ql = desc_low(sQ(qs), 16), kl = desc_low(sK(st), 16);
-            if (elect_one()) {
+        // =============================================================== MMA issuer
+        if (elect_one()) {
+            constexpr uint32_t idesc_s = instr_desc(kHalf, 0);
+            constexpr uint32_t idesc_o = instr_desc(D, 1);
+            Ring<C::kNQ> q;
+            Ring<C::kNKV> k, v;
+            uint32_t par = 0, oph = 1;               // bit p: phase of the weights in slot p; phase of o_free to wait for
+            bool ok = true;
+            for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
+                const int item = item_of_round(a.total_items, round);
+                if (item < 0) continue;
+                const Item c = decode(a, item);
+                if (c.n == 0) continue;
+                const uint32_t q_low = desc_low(sQ(q.st), 16);
+                // scores of the half block in K's stage, chain ch, into slot p
+                auto scores = [&](int ch, int p, uint32_t k_low) {
 #pragma unroll
-                for (int kb = 0; kb < C::kd / 16; ++kb) {
-                    const uint32_t off = map_k_off<D>(c, kb, kSlab) >> 4;
-                    mma_ss(tmem_base + C::kColS + c * 128, ql + off, kl + off, idesc_s, kb > 0);
-                }
-                tc_commit(s_full(c));
-            }
-            __syncwarp();
-        };
-        for (long long round = 0; ok && round * gridDim.x < a.total_items; ++round) {
-            const long long item = item_of_round(a, round);
-            if (item < 0) continue;
-            const Item c = decode(a, item);
-            if (c.nblocks == 0) continue;
-            const int qs = ic % C::kNQ;
-            ok = warp_wait(q_full(qs), (ic / C::kNQ) & 1, 0xE10, abort_flag);
-            if (ok) ok = warp_wait(k_full(g % C::kNKV), (g / C::kNKV) & 1, 0xE11, abort_flag);
-            if (!ok) break;
-            tc_fence_after();
-            scores(0, qs, g % C::kNKV);
-            scores(1, qs, g % C::kNKV);
-            for (int j = 0; j < c.nblocks; ++j, ++g, ++pc) {
-                const int st = g % C::kNKV, nx = (g + 1) % C::kNKV;
-                const bool more = j + 1 < c.nblocks;
-                ok = warp_wait(v_full(st), (g / C::kNKV) & 1, 0xE12, abort_flag);
-                if (ok && more) ok = warp_wait(k_full(nx), ((g + 1) / C::kNKV) & 1, 0xE13, abort_flag);
-                if (!ok) break;
-                const int keys = min(kRows, c.keys_end - kRows * j);
-                const int ksteps = (keys + 15) >> 4;
-                if (c.sp.kl < a.Nk && c.sp.kl - kRows * j < 16 * ksteps) {
-                    zero_rows(sV(st), kSlab, C::kSlabs, c.sp.kl - kRows * j, 16 * ksteps);
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                }
-#pragma unroll
-                for (int ch = 0; ch < 2; ++ch) {
-                    ok = warp_wait(p_full(ch), pc & 1, 0xE14, abort_flag);
-                    if (ok && j == 0 && ch == 0) ok = warp_wait(o_free, (ic & 1) ^ 1, 0xE15, abort_flag);
+                    for (int kb = 0; kb < C::kd / 16; ++kb)
+                        mma_ss(tmem_base + ch * 128 + p * 64, q_low + map_k_off<D>(ch, kb, kSlab) / 16,
+                               k_low + map_k_off<D>(ch, kb, kHSlab) / 16, idesc_s, kb > 0);
+                    tc_commit(s_full(ch, p));
+                };
+                ok = mbar_wait_abortable(q_full(q.st), q.ph, 0xE10, abort_flag);
+                for (int j = 0; ok && j < 2 && j < c.n; ++j) {
+                    ok = mbar_wait_abortable(k_full(k.st), k.ph, 0xE11, abort_flag);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t vl = desc_low(sV(st), kSlab), o = tmem_base + C::kColO + ch * 128, w = tmem_base + C::kColS + ch * 128;
-                    const uint32_t first = j > 0 ? 1u : 0u;
-                    if (elect_one()) {
+                    scores(0, j, desc_low(sK(k.st), 16));
+                    scores(1, j, desc_low(sK(k.st), 16));
+                    tc_commit(k_free(k.st));
+                    k.next();
+                }
+                for (int j = 0; ok && j < c.n; ++j) {
+                    const int p = j & 1;
+                    const bool more = j + 2 < c.n;
+                    ok = mbar_wait_abortable(v_full(v.st), v.ph, 0xE12, abort_flag);
+                    if (ok && more) ok = mbar_wait_abortable(k_full(k.st), k.ph, 0xE13, abort_flag);
+                    if (!ok) break;
+                    const int ksteps = min(kHalf / 16, (c.keys_end - kHalf * j + 15) >> 4);
+                    if (c.sp.kl < a.Nk && c.sp.kl < kHalf * j + 16 * ksteps) {
+                        zero_rows(sV(v.st), kHSlab, C::kSlabs, c.sp.kl - kHalf * j, 16 * ksteps);
+                        fence_proxy_async_smem();
+                    }
+                    const uint32_t v_low = desc_low(sV(v.st), kHSlab), k_low = desc_low(sK(k.st), 16), first = j > 0 ? 1u : 0u;
+#pragma unroll
+                    for (int ch = 0; ch < 2; ++ch) {
+                        ok = mbar_wait_abortable(p_full(ch, p), (par >> p) & 1, 0xE14, abort_flag);
+                        if (ok && j == 0 && ch == 0) ok = mbar_wait_abortable(o_free, oph, 0xE15, abort_flag);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint32_t w = tmem_base + ch * 128 + p * 64;
                         // (weights beyond ksteps are zeros that nothing has to multiply)
 #pragma unroll
-                        for (int kb = 0; kb < kRows / 16; ++kb)
-                            if (kb < ksteps) mma_ts(o, w + kb * 8, vl + 128u * kb, idesc_o, kb > 0 ? 1u : first);
-                        if (ch == 1) tc_commit(kv_free(st));
-                        if (!more) tc_commit(o_full(ch));
-                        if (!more && ch == 1) tc_commit(q_free(qs));
+                        for (int kb = 0; kb < kHalf / 16; ++kb)
+                            if (kb < ksteps) mma_ts(tmem_base + C::kColO + ch * 128, w + kb * 8, v_low + 128u * kb, idesc_o, kb > 0 ? 1u : first);
+                        tc_commit(pv_done(ch));
+                        if (j + 1 == c.n) tc_commit(o_full(ch));
+                        if (ch == 1) tc_commit(v_free(v.st));
+                        if (more) scores(ch, p, k_low);
                     }
-                    __syncwarp();
-                    if (more) scores(ch, qs, nx);
+                    if (!ok) break;
+                    v.next();
+                    if (more) {
+                        tc_commit(k_free(k.st));
+                        k.next();
+                    }
+                    par ^= 1u << p;
                 }
-                if (!ok) break;
+                // every score of the item has been issued
+                tc_commit(q_free(q.st));
+                q.next();
+                oph ^= 1u;
             }
-            ++ic;
         }
     } else if (warp >= 4) {
         // =============================================================== softmax, epilogue
     
         const int ch = (warp - 4) >> 2, wq = warp & 3;
         const uint32_t tmem_lane = tmem_base + ((uint32_t)(wq * 32) << 16);
-        const uint32_t s_col = tmem_lane + C::kColS + ch * 128;
+        const uint32_t s_col = tmem_lane + ch * 128;
         const uint32_t o_col = tmem_lane + C::kColO + ch * 128;
         const int r = wq * 32 + lane;
         bool ok = true;
-        uint32_t ic = 0, sc = 0;
-        for (long long round = 0; ok && round * gridDim.x < a.total_items; ++round) {
-            const long long item = item_of_round(a, round);
+        uint32_t ic = 0, sc = 0, par = 0;               // items, half blocks so far; bit p: phase of the scores in slot p
+        for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
+            const int item = item_of_round(a.total_items, round);
             if (item < 0) continue;
             const Item c = decode(a, item);
             const int t = c.t0 + r;
             const int row_keys = c.sp.keys(t, a.causal);
             float m = -INFINITY, l = 0.f;               // running maximum (scaled, log2) and sum
-            for (int j = 0; j < c.nblocks; ++j, ++sc) {
-                ok = warp_wait(s_full(ch), sc & 1, 0xF10, abort_flag);
+            for (int j = 0; j < c.n; ++j, ++sc) {
+                const int p = j & 1;
+                const uint32_t col = s_col + 64 * p;
+                ok = warp_wait(s_full(ch, p), (par >> p) & 1, 0xF10, abort_flag);
+                par ^= 1u << p;
                 if (!ok) break;
                 tc_fence_after();
-                // pass over the scores for the row maximum; they are read again for the weights (128 of them held
-                // across the rescaling would spill)
-                const int c_hi = row_keys - kRows * j;
-                const bool whole = __all_sync(0xffffffffu, c_hi >= kRows);
-                float bm0 = -INFINITY, bm1 = -INFINITY, bm2 = -INFINITY, bm3 = -INFINITY;
-                uint32_t v[2][32];
-                tmem_ld32_nowait(s_col, v[0]);
+                uint32_t v[64];
+                tmem_ld32_nowait(col, v);
+                tmem_ld32_nowait(col + 32, v + 32);
+                tmem_ld_wait();
+                const int c_hi = row_keys - kHalf * j;
+                if (!__all_sync(0xffffffffu, c_hi >= kHalf)) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    tmem_ld_wait();
-                    if (i < 3) tmem_ld32_nowait(s_col + 32 * (i + 1), v[(i + 1) & 1]);
-                    uint32_t *x = v[i & 1];
-                    if (!whole) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (32 * i + e >= c_hi) x[e] = 0xFF800000u;      // -inf
-                    }
-#pragma unroll
-                    for (int e = 0; e < 32; e += 8) {
-                        bm0 = fmaxf(bm0, fmaxf(__uint_as_float(x[e]), __uint_as_float(x[e + 1])));
-                        bm1 = fmaxf(bm1, fmaxf(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3])));
-                        bm2 = fmaxf(bm2, fmaxf(__uint_as_float(x[e + 4]), __uint_as_float(x[e + 5])));
-                        bm3 = fmaxf(bm3, fmaxf(__uint_as_float(x[e + 6]), __uint_as_float(x[e + 7])));
-                    }
+                    for (int e = 0; e < 64; ++e)
+                        if (e >= c_hi) v[e] = 0xFF800000u;      // -inf
                 }
-                const float bm = fmaxf(fmaxf(bm0, bm1), fmaxf(bm2, bm3)) * a.scale_log2;
+                float b0 = -INFINITY, b1 = -INFINITY, b2 = -INFINITY, b3 = -INFINITY;
+#pragma unroll
+                for (int e = 0; e < 64; e += 8) {
+                    b0 = fmaxf(b0, fmaxf(__uint_as_float(v[e]), __uint_as_float(v[e + 1])));
+                    b1 = fmaxf(b1, fmaxf(__uint_as_float(v[e + 2]), __uint_as_float(v[e + 3])));
+                    b2 = fmaxf(b2, fmaxf(__uint_as_float(v[e + 4]), __uint_as_float(v[e + 5])));
+                    b3 = fmaxf(b3, fmaxf(__uint_as_float(v[e + 6]), __uint_as_float(v[e + 7])));
+                }
+                const float bm = fmaxf(fmaxf(b0, b1), fmaxf(b2, b3)) * a.scale_log2;
                 if (__any_sync(0xffffffffu, bm > m + 8.f)) {
-                    // the first block, or the maximum has outgrown the reference: move it, rescale what was summed so far
+                    // the first half block, or the maximum has outgrown the reference: move it, rescale what was summed so far
                     const float mn = fmaxf(m, bm);
                     const float alpha = m == -INFINITY ? 0.f : fast_exp2(m - mn);
                     l *= alpha;
+                    m = mn;
                     if (j > 0) {
-                        // (S of this block was issued behind the previous value product: that one is complete)
+                        // (the scores of this half block were issued behind the value product before the last: only the last
+                        // one's phase can be open)
+                        ok = warp_wait(pv_done(ch), (sc - 1) & 1, 0xF14, abort_flag);
+                        if (!ok) break;
+                        tc_fence_after();
 #pragma unroll 1
                         for (int i = 0; i < D / 32; ++i) {
                             uint32_t o[32];
@@ -325,40 +315,24 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                             tmem_st32(o_col + 32 * i, o);
                         }
                     }
-                    m = mn;
                 }
                 const float ref = m == -INFINITY ? 0.f : m;
                 const float2 nref = make_float2(-ref, -ref), sl2 = make_float2(a.scale_log2, a.scale_log2);
                 float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
-                tmem_ld32_nowait(s_col, v[0]);
+                uint32_t pk[32];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    tmem_ld_wait();
-                    if (i < 3) tmem_ld32_nowait(s_col + 32 * (i + 1), v[(i + 1) & 1]);
-                    uint32_t *x = v[i & 1];
-                    if (!whole) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (32 * i + e >= c_hi) x[e] = 0xFF800000u;
-                    }
-                    uint32_t pk[16];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        float2 y = fma2(make_float2(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), sl2, nref);
-                        y.x = fast_exp2(y.x);
-                        y.y = fast_exp2(y.y);
-                        pk[e] = pack_bf16x2(y.x, y.y);
-                        if (e & 1) sum1 = add2(sum1, y); else sum0 = add2(sum0, y);
-                    }
-                    // (columns 16 i .. of the scores have been read: the next chunk, at 32 (i + 1), has been waited for or
-                    // lies behind)
-                    tmem_st16(s_col + 16 * i, pk);
+                for (int e = 0; e < 32; ++e) {
+                    float2 y = fma2(make_float2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), sl2, nref);
+                    y = e % 4 == 3 ? exp2_poly(y) : exp2_mufu(y);
+                    pk[e] = pack_bf16x2(y.x, y.y);
+                    if (e & 1) sum1 = add2(sum1, y); else sum0 = add2(sum0, y);
                 }
+                tmem_st32(col, pk);
                 l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_full(ch));
+                if (lane == 0) mbar_arrive(p_full(ch, p));
             }
             if (!ok) break;
 
@@ -367,7 +341,7 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             const float inv = l > 0.f || l != l ? 1.f / l : 0.f;         // (NaN stays NaN)
             const long long row = ((long long)c.b * a.H + c.h) * a.Nq + t;
             float i1 = 0.f, i2 = 0.f;
-            if (c.nblocks > 0) {
+            if (c.n > 0) {
                 // (the other chain has read the last item's numbers: no value product of this item starts before)
                 s_inv[ch * kRows + r] = inv;
                 __syncwarp();
@@ -386,7 +360,7 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 #pragma unroll 1
             for (int i = ch * (D / 64); i < (ch + 1) * (D / 64); ++i) {
                 uint32_t o1[32], o2[32];
-                // (an item without blocks reads what the last one left, and drops it)
+                // (an item without keys reads what the last one left, and drops it)
                 tmem_ld32_nowait(tmem_lane + C::kColO + 32 * i, o1);
                 tmem_ld32_nowait(tmem_lane + C::kColO + 128 + 32 * i, o2);
                 tmem_ld_wait();
@@ -436,7 +410,7 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             }
             tc_fence_before();
             __syncwarp();
-            if (c.nblocks > 0 && lane == 0) mbar_arrive(o_free);
+            if (c.n > 0 && lane == 0) mbar_arrive(o_free);
         }
     }
 
@@ -454,12 +428,14 @@ int launch_d(const DiffProblem &p) {
     CUtensorMap mq, mk, mv;
     int rc;
     if ((rc = make_strided_map(&mq, p.q, &p.sq.b, p.B, p.H, p.Nq, D, kRows)) != TA_OK) return rc;
-    if ((rc = make_strided_map(&mk, p.k, &p.sk.b, p.B, p.H_kv, p.Nk, D, kRows)) != TA_OK) return rc;
-    if ((rc = make_strided_map(&mv, p.v, &p.sv.b, p.B, p.H_kv, p.Nk, D, kRows)) != TA_OK) return rc;
+    if ((rc = make_strided_map(&mk, p.k, &p.sk.b, p.B, p.H_kv, p.Nk, D, kHalf)) != TA_OK) return rc;
+    if ((rc = make_strided_map(&mv, p.v, &p.sv.b, p.B, p.H_kv, p.Nk, D, kHalf)) != TA_OK) return rc;
     TcArgs a = {};
     a.B = p.B; a.H = p.H; a.H_kv = p.H_kv; a.g = p.H / p.H_kv; a.Nq = p.Nq; a.Nk = p.Nk; a.causal = p.causal;
     a.qtiles = (p.Nq + kRows - 1) / kRows;
-    a.total_items = (long long)p.B * p.H * a.qtiles;
+    const long long items = (long long)p.B * p.H * a.qtiles;
+    if (items > 0x3FFFFFFFll) return TA_ERR_TOO_LARGE;
+    a.total_items = (int)items;
     // K and V of all heads against the 126 MB L2
     a.tile_major = 2ull * p.B * p.H_kv * p.Nk * D * 2 <= (96ull << 20) ? 1 : 0;
     a.scale_log2 = p.scale * 1.4426950408889634f;

@@ -37,7 +37,8 @@ __device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_
         ::"r"(d_tmem), "r"(a_tmem), "r"(b_low), "r"(idesc), "r"(accumulate), "r"(kDescHigh)
         : "memory");
 }
-// true in one lane of the (converged) warp
+// true in one lane of the (converged) warp: a role of one thread runs in it.  (Waiting with the whole warp and electing a
+// lane per product cost 1800 cycles of instructions per half tile, where the products take 900.)
 __device__ __forceinline__ bool elect_one() {
     uint32_t p;
     asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n selp.u32 %0, 1, 0, q;\n}" : "=r"(p));
@@ -79,6 +80,30 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t *v) {
         : "memory");
 }
 
+// 2^x on the multiply-add pipes, for a share of the exponentials: the special-function unit takes 16 a cycle and SM, and
+// alone would bound these kernels.  x = n + f, n the nearest whole number (left in the low bits of x + 1.5 * 2^23),
+// 2^f on [-1/2, 1/2] by the polynomial of degree 4 with the least largest relative error (2.6e-6, from Remez' exchange;
+// 4e-8 on average), n added to the exponent.  Below 2^-126 the result is 0 or denormal.  NaN stays non-finite.
+__device__ __forceinline__ float clamp_exp(float x) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(x), "f"(-126.f));
+    return y;
+}
+__device__ __forceinline__ float2 exp2_poly(float2 x) {
+    x.x = clamp_exp(x.x);
+    x.y = clamp_exp(x.y);
+    const float2 t = add2(x, make_float2(12582912.f, 12582912.f));
+    const float2 n = add2(t, make_float2(-12582912.f, -12582912.f));
+    const float2 f = fma2(n, make_float2(-1.f, -1.f), x);
+    float2 p = fma2(f, make_float2(9.570102207e-3f, 9.570102207e-3f), make_float2(5.591785908e-2f, 5.591785908e-2f));
+    p = fma2(p, f, make_float2(2.402474433e-1f, 2.402474433e-1f));
+    p = fma2(p, f, make_float2(6.931217909e-1f, 6.931217909e-1f));
+    p = fma2(p, f, make_float2(9.999992847e-1f, 9.999992847e-1f));
+    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
+                       __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
+}
+__device__ __forceinline__ float2 exp2_mufu(float2 x) { return make_float2(fast_exp2(x.x), fast_exp2(x.y)); }
+
 // 16 columns -> registers, without the wait; registers -> 8 columns
 __device__ __forceinline__ void tmem_ld16_nowait(uint32_t taddr, uint32_t *v) {
     __syncwarp();
@@ -110,13 +135,51 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t *v) {
                  : "memory");
 }
 
-// Zeroes rows [r0, r1) of a tile in shared memory (kSlabs slabs of 128-byte rows); the whole warp takes part.  For rows the
-// tensor holds but the call's lengths do not count: whatever stands there must not meet a weight of 0 in a product.
+// Zeroes rows [r0, r1), fewer than 16, of a tile in shared memory (slabs of 128-byte rows), by one thread.  For rows the
+// tensor holds but the call's lengths do not count, in the last step of 16 a product takes: whatever stands there must not
+// meet a weight of 0.
 __device__ __forceinline__ void zero_rows(uint32_t tile, uint32_t slab_bytes, int slabs, int r0, int r1) {
-    const int lane = threadIdx.x & 31;
     for (int s = 0; s < slabs; ++s)
-        for (int i = r0 * 8 + lane; i < r1 * 8; i += 32) st_shared_v4(tile + s * slab_bytes + (uint32_t)i * 16u, 0, 0, 0, 0);
+        for (int i = r0 * 8; i < r1 * 8; ++i) st_shared_v4(tile + s * slab_bytes + (uint32_t)i * 16u, 0, 0, 0, 0);
 }
+
+// A ring's next stage and the phase its barriers are in.
+template <int kStages>
+struct Ring {
+    int st = 0;
+    uint32_t ph = 0;
+    __device__ __forceinline__ void next() {
+        if (++st == kStages) {
+            st = 0;
+            ph ^= 1u;
+        }
+    }
+};
+
+// The item of a CTA's k-th round: forth and back over the CTAs, so that long and short items pair up; -1: none.  (Rounds and
+// items fit 32 bits: the launchers see to it.)
+__device__ __forceinline__ int item_of_round(int total_items, int k) {
+    const int g = (int)gridDim.x, b = (int)blockIdx.x;
+    const int item = k * g + ((k & 1) ? g - 1 - b : b);
+    return item < total_items ? item : -1;
+}
+
+// Remembers the copies a producer has started, so that they can be waited for when it gives up.
+struct Armed {
+    uint32_t mask = 0, par = 0;
+    __device__ __forceinline__ void arm(int bar, uint32_t parity) {
+        mask |= 1u << bar;
+        par = parity ? (par | 1u << bar) : (par & ~(1u << bar));
+    }
+    __device__ __forceinline__ void drain(uint32_t bar0, int bars) const {
+        const unsigned long long t0 = globaltimer_ns();
+        for (int i = 0; i < bars; ++i) {
+            if (!(mask & (1u << i))) continue;
+            while (!mbar_try_wait(bar0 + 8u * (uint32_t)i, (par >> i) & 1u) && globaltimer_ns() - t0 < 10000000ull) {
+            }
+        }
+    }
+};
 
 // warp-uniform bounded wait of a whole warp
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, uint32_t where, volatile uint32_t *abort_flag) {

@@ -48,41 +48,18 @@ struct BwdArgs {
 // scores that the same warps have read.
 __device__ __forceinline__ constexpr uint32_t weight_col(int kb) { return (uint32_t)(kb >> 1) * 32u + (uint32_t)(kb & 1) * 8u; }
 
-// the item of a CTA's k-th round: forth and back over the CTAs, so that long and short items pair up; -1: none
-// (rounds and items fit 32 bits: launch_d sees to it)
-__device__ __forceinline__ int item_of_round(const BwdArgs &a, int k) {
-    const int g = (int)gridDim.x, b = (int)blockIdx.x;
-    const int item = k * g + ((k & 1) ? g - 1 - b : b);
-    return item < a.total_items ? item : -1;
-}
-
-// Remembers the copies a producer has started, so that they can be waited for when it gives up.
-struct Armed {
-    uint32_t mask = 0, par = 0;
-    __device__ __forceinline__ void arm(int bar, uint32_t parity) {
-        mask |= 1u << bar;
-        par = parity ? (par | 1u << bar) : (par & ~(1u << bar));
-    }
-    __device__ __forceinline__ void drain(uint32_t bar0, int bars) const {
-        const unsigned long long t0 = globaltimer_ns();
-        for (int i = 0; i < bars; ++i) {
-            if (!(mask & (1u << i))) continue;
-            while (!mbar_try_wait(bar0 + 8u * (uint32_t)i, (par >> i) & 1u) && globaltimer_ns() - t0 < 10000000ull) {
-            }
-        }
-    }
-};
-
 // ------------------------------------------------------------------ dQ and dlambda: one query tile, all its keys
 
 template <int D>
 struct DqCfg {
     static constexpr int kSlabs = D / 64, kd = D / 2;
     static constexpr uint32_t kSlab = kRows * 128, kTile = kSlabs * kSlab;
-    static constexpr int kNKV = D == 128 ? 2 : 4;
-    static constexpr uint32_t kOffQ = 0, kOffG = kTile, kOffK = 2 * kTile, kOffV = kOffK + kNKV * kTile;
-    static constexpr uint32_t kOffBar = kOffV + kNKV * kTile;
-    static constexpr int kNumBars = 2 + 3 * kNKV + 6;
+    // K, V in stages of 64 keys: five of them cover the way to L2 and back, two of 128 keys did not
+    static constexpr uint32_t kHSlab = kHalf * 128, kHTile = kSlabs * kHSlab;
+    static constexpr int kNKV = D == 128 ? 5 : 6;
+    static constexpr uint32_t kOffQ = 0, kOffG = kTile, kOffK = 2 * kTile, kOffV = kOffK + kNKV * kHTile;
+    static constexpr uint32_t kOffBar = kOffV + kNKV * kHTile;
+    static constexpr int kNumBars = 2 + 2 * kNKV + 6;
     static constexpr uint32_t kSmem = kOffBar + kNumBars * 8 + 16 + 1024;
     // per chain (64 keys): S_1, S_2 (dS_c over their first 32 columns), dA; then dQ
     static constexpr uint32_t kColChain = 192, kColDQ = 384;
@@ -125,16 +102,15 @@ diff_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     const uint32_t s0 = smem_u32(smem);
     const uint32_t sQ = s0 + C::kOffQ, sG = s0 + C::kOffG;
-    auto sK = [&](int i) { return s0 + C::kOffK + (uint32_t)i * C::kTile; };
-    auto sV = [&](int i) { return s0 + C::kOffV + (uint32_t)i * C::kTile; };
+    auto sK = [&](int i) { return s0 + C::kOffK + (uint32_t)i * C::kHTile; };
+    auto sV = [&](int i) { return s0 + C::kOffV + (uint32_t)i * C::kHTile; };
     const uint32_t bar0 = s0 + C::kOffBar;
     auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
-    // barriers 0 .. 2 kNKV are those copies complete on
+    // barriers 0 .. kNKV are those copies complete on
     const uint32_t q_full = bar(0);
-    auto k_full = [&](int i) { return bar(1 + i); };
-    auto v_full = [&](int i) { return bar(1 + C::kNKV + i); };
-    auto kv_free = [&](int i) { return bar(1 + 2 * C::kNKV + i); };
-    constexpr int kB = 1 + 3 * C::kNKV;
+    auto kv_full = [&](int i) { return bar(1 + i); };
+    auto kv_free = [&](int i) { return bar(1 + C::kNKV + i); };
+    constexpr int kB = 1 + 2 * C::kNKV;
     const uint32_t q_free = bar(kB);
     auto s_full = [&](int c) { return bar(kB + 1 + c); };      // S_1, S_2, dA of chain c complete
     auto ds_full = [&](int c) { return bar(kB + 3 + c); };     // dS_1, dS_2 of chain c written (8 warps)
@@ -161,127 +137,106 @@ diff_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
 
     if (warp == 0) {
         // =============================================================== TMA producer
-        if (lane == 0) {
-            uint32_t ic = 0, g = 0;
+        if (elect_one()) {
+            uint32_t qph = 1;
+            Ring<C::kNKV> kv;
             Armed armed;
             bool ok = true;
             for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
-                const int item = item_of_round(a, round);
+                const int item = item_of_round(a.total_items, round);
                 if (item < 0) continue;
                 const DqItem c = decode_dq(a, item);
                 if (c.nhalf == 0) continue;
-                ok = mbar_wait_abortable(q_free, (ic & 1) ^ 1, 0x110, abort_flag);
-                if (!ok) break;
-                mbar_expect_tx(q_full, 2 * C::kTile);
-                armed.arm(0, ic & 1);
-                ++ic;
-#pragma unroll
-                for (int s = 0; s < C::kSlabs; ++s) {
-                    tma_load_5d(sQ + s * C::kSlab, &map_q, q_full, 64 * s, c.t0, 0, c.h, c.b);
-                    tma_load_5d(sG + s * C::kSlab, &map_g, q_full, 64 * s, c.t0, 0, c.h, c.b);
-                }
-                for (int j = 0; 2 * j < c.nhalf; ++j, ++g) {
-                    const int st = g % C::kNKV;
-                    const uint32_t par = (g / C::kNKV) & 1;
-                    ok = mbar_wait_abortable(kv_free(st), par ^ 1, 0x111, abort_flag);
+                // (the first keys of an item are requested while the last item's products still read its Q and dO)
+                const int early = min(3, c.nhalf);
+                for (int j = 0; j < c.nhalf; ++j, kv.next()) {
+                    ok = mbar_wait_abortable(kv_free(kv.st), kv.ph ^ 1, 0x111, abort_flag);
                     if (!ok) break;
-                    mbar_expect_tx(k_full(st), C::kTile);
-                    armed.arm(1 + st, par);
-#pragma unroll
-                    for (int s = 0; s < C::kSlabs; ++s)
-                        tma_load_5d(sK(st) + s * C::kSlab, &map_k, k_full(st), 64 * s, kRows * j, 0, c.hk, c.b);
-                    mbar_expect_tx(v_full(st), C::kTile);
-                    armed.arm(1 + C::kNKV + st, par);
-#pragma unroll
-                    for (int s = 0; s < C::kSlabs; ++s)
-                        tma_load_5d(sV(st) + s * C::kSlab, &map_v, v_full(st), 64 * s, kRows * j, 0, c.hk, c.b);
+                    mbar_expect_tx(kv_full(kv.st), 2 * C::kHTile);
+                    armed.arm(1 + kv.st, kv.ph);
+                    tma_load_5d(sK(kv.st), &map_k, kv_full(kv.st), 0, kHalf * j, 0, c.hk, c.b);
+                    tma_load_5d(sV(kv.st), &map_v, kv_full(kv.st), 0, kHalf * j, 0, c.hk, c.b);
+                    if (j + 1 == early) {
+                        ok = mbar_wait_abortable(q_free, qph, 0x110, abort_flag);
+                        if (!ok) break;
+                        mbar_expect_tx(q_full, 2 * C::kTile);
+                        armed.arm(0, qph ^ 1);
+                        qph ^= 1;
+                        tma_load_5d(sQ, &map_q, q_full, 0, c.t0, 0, c.h, c.b);
+                        tma_load_5d(sG, &map_g, q_full, 0, c.t0, 0, c.h, c.b);
+                    }
                 }
             }
-            if (!ok) armed.drain(bar0, 1 + 2 * C::kNKV);
+            if (!ok) armed.drain(bar0, 1 + C::kNKV);
         }
     } else if (warp == 1) {
         // =============================================================== MMA issuer
-        constexpr uint32_t idesc_s = instr_desc(kHalf, 0);
-        constexpr uint32_t idesc_q = instr_desc(C::kd, 1);
-        const uint32_t q_low = desc_low(sQ, 16), g_low = desc_low(sG, 16);
-        uint32_t ic = 0, g0 = 0, sc[2] = {0, 0};     // items, key blocks before this item, half tiles of each chain
-        bool ok = true;
-        // S_1, S_2, dA of half tile i of the item (keys 64 i ..)
-        auto scores = [&](const DqItem &c, int i) {
-            const uint32_t g = g0 + (uint32_t)(i >> 1);
-            const int st = g % C::kNKV, ch = i & 1;
-            bool fine = true;
-            if (ch == 0) {
-                fine = warp_wait(k_full(st), (g / C::kNKV) & 1, 0x120, abort_flag);
-                if (fine) fine = warp_wait(v_full(st), (g / C::kNKV) & 1, 0x121, abort_flag);
-                if (!fine) return false;
-                // keys the tensor has but the call does not count: they meet dS = 0 in the product for dQ
-                if (c.sp.kl < a.Nk && c.sp.kl < kRows * (i >> 1) + kRows) {
-                    zero_rows(sK(st), C::kSlab, C::kSlabs, c.sp.kl - kRows * (i >> 1), kRows);
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                }
-            }
-            tc_fence_after();
-            const uint32_t rows = (uint32_t)ch * kHalf * 128u;
-            const uint32_t col = tmem_base + ch * C::kColChain;
-            const uint32_t kl = desc_low(sK(st) + rows, 16), vl = desc_low(sV(st) + rows, 16);
-            if (elect_one()) {
+        if (elect_one()) {
+            constexpr uint32_t idesc_s = instr_desc(kHalf, 0);
+            constexpr uint32_t idesc_q = instr_desc(C::kd, 1);
+            const uint32_t q_low = desc_low(sQ, 16), g_low = desc_low(sG, 16);
+            Ring<C::kNKV> kv, kq;                    // stage of the next scores, of the next product for dQ
+            uint32_t qph = 0, par = 0;               // bit ch: phase of chain ch's dS
+            bool ok = true;
+            // S_1, S_2, dA of the next half tile, into chain ch
+            auto scores = [&](int ch) {
+                if (!mbar_wait_abortable(kv_full(kv.st), kv.ph, 0x120, abort_flag)) return false;
+                tc_fence_after();
+                const uint32_t col = tmem_base + ch * C::kColChain;
+                const uint32_t kl = desc_low(sK(kv.st), 16), vl = desc_low(sV(kv.st), 16);
 #pragma unroll
                 for (int m = 0; m < 2; ++m)
 #pragma unroll
-                    for (int kb = 0; kb < C::kd / 16; ++kb) {
-                        const uint32_t off = map_k_off<D>(m, kb, C::kSlab) >> 4;
-                        mma_ss(col + 64 * m, q_low + off, kl + off, idesc_s, kb > 0);
-                    }
+                    for (int kb = 0; kb < C::kd / 16; ++kb)
+                        mma_ss(col + 64 * m, q_low + (map_k_off<D>(m, kb, C::kSlab) >> 4), kl + (map_k_off<D>(m, kb, C::kHSlab) >> 4),
+                               idesc_s, kb > 0);
 #pragma unroll
-                for (int kb = 0; kb < D / 16; ++kb) {
-                    const uint32_t off = ((kb >> 2) * C::kSlab + (kb & 3) * 32) >> 4;
-                    mma_ss(col + 128, g_low + off, vl + off, idesc_s, kb > 0);
-                }
+                for (int kb = 0; kb < D / 16; ++kb)
+                    mma_ss(col + 128, g_low + (((kb >> 2) * C::kSlab + (kb & 3) * 32) >> 4),
+                           vl + (((kb >> 2) * C::kHSlab + (kb & 3) * 32) >> 4), idesc_s, kb > 0);
                 tc_commit(s_full(ch));
-            }
-            __syncwarp();
-            return true;
-        };
-        for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
-            const int item = item_of_round(a, round);
-            if (item < 0) continue;
-            const DqItem c = decode_dq(a, item);
-            if (c.nhalf == 0) continue;
-            ok = warp_wait(q_full, ic & 1, 0x122, abort_flag);
-            if (ok) ok = scores(c, 0);
-            if (ok && c.nhalf > 1) ok = scores(c, 1);
-            for (int i = 0; ok && i < c.nhalf; ++i) {
-                const int ch = i & 1;
-                const uint32_t g = g0 + (uint32_t)(i >> 1);
-                const int st = g % C::kNKV;
-                ok = warp_wait(ds_full(ch), sc[ch] & 1, 0x123, abort_flag);
-                ++sc[ch];
-                if (ok && i == 0) ok = warp_wait(dq_free, (ic & 1) ^ 1, 0x124, abort_flag);
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t col = tmem_base + ch * C::kColChain;
-                const uint32_t kl = desc_low(sK(st) + (uint32_t)ch * kHalf * 128u, C::kSlab);
-                const uint32_t first = i > 0 ? 1u : 0u;
-                if (elect_one()) {
+                kv.next();
+                return true;
+            };
+            for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
+                const int item = item_of_round(a.total_items, round);
+                if (item < 0) continue;
+                const DqItem c = decode_dq(a, item);
+                if (c.nhalf == 0) continue;
+                ok = mbar_wait_abortable(q_full, qph, 0x122, abort_flag);
+                if (ok) ok = scores(0);
+                if (ok && c.nhalf > 1) ok = scores(1);
+                for (int i = 0; ok && i < c.nhalf; ++i) {
+                    const int ch = i & 1;
+                    ok = mbar_wait_abortable(ds_full(ch), (par >> ch) & 1, 0x123, abort_flag);
+                    par ^= 1u << ch;
+                    if (ok && i == 0) ok = mbar_wait_abortable(dq_free, qph ^ 1, 0x124, abort_flag);
+                    if (!ok) break;
+                    const int ksteps = min(kHalf / 16, (c.keys_end - kHalf * i + 15) >> 4);
+                    if (c.sp.kl < a.Nk && c.sp.kl < kHalf * i + 16 * ksteps) {
+                        zero_rows(sK(kq.st), C::kHSlab, C::kSlabs, c.sp.kl - kHalf * i, 16 * ksteps);
+                        fence_proxy_async_smem();
+                    }
+                    tc_fence_after();
+                    const uint32_t col = tmem_base + ch * C::kColChain, first = i > 0 ? 1u : 0u;
+                    const uint32_t kl = desc_low(sK(kq.st), C::kHSlab);
 #pragma unroll
                     for (int m = 0; m < 2; ++m)
 #pragma unroll
                         for (int kb = 0; kb < kHalf / 16; ++kb)
-                            mma_ts(tmem_base + C::kColDQ + m * C::kd, col + 64 * m + weight_col(kb),
-                                   kl + ((map_n_off<D>(m, C::kSlab) + 16u * kb * 128u) >> 4), idesc_q, kb > 0 ? 1u : first);
-                    if (ch == 1 || i + 1 == c.nhalf) tc_commit(kv_free(st));
+                            if (kb < ksteps)
+                                mma_ts(tmem_base + C::kColDQ + m * C::kd, col + 64 * m + weight_col(kb),
+                                       kl + ((map_n_off<D>(m, C::kHSlab) + 16u * kb * 128u) >> 4), idesc_q, kb > 0 ? 1u : first);
+                    tc_commit(kv_free(kq.st));
+                    kq.next();
                     if (i + 1 == c.nhalf) {
                         tc_commit(dq_full);
                         tc_commit(q_free);
                     }
+                    if (i + 2 < c.nhalf) ok = scores(ch);
                 }
-                __syncwarp();
-                if (i + 2 < c.nhalf) ok = scores(c, i + 2);
+                qph ^= 1u;
             }
-            g0 += (uint32_t)((c.nhalf + 1) >> 1);
-            ++ic;
         }
     } else if (warp >= 4) {
         // =============================================================== weights, dS, epilogue
@@ -292,7 +247,7 @@ diff_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         bool ok = true;
         uint32_t ic = 0, sc = 0;
         for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
-            const int item = item_of_round(a, round);
+            const int item = item_of_round(a.total_items, round);
             if (item < 0) continue;
             const DqItem c = decode_dq(a, item);
             const int t = c.t0 + r;
@@ -494,68 +449,69 @@ diff_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     if (warp < 4) {
         if (warp == 0) {
             // =========================================================== TMA producer
-            if (lane == 0) {
-                uint32_t ic = 0, g = 0;
+            if (elect_one()) {
+                uint32_t kph = 1;
+                Ring<C::kStages> q;
                 Armed armed;
                 bool ok = true;
                 for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
-                    const int item = item_of_round(a, round);
+                    const int item = item_of_round(a.total_items, round);
                     if (item < 0) continue;
                     const DkvItem c = decode_dkv(a, item);
                     if (c.n == 0) continue;
-                    ok = mbar_wait_abortable(kv_free, (ic & 1) ^ 1, 0x210, abort_flag);
-                    if (!ok) break;
-                    mbar_expect_tx(kv_full, 2 * C::kTile);
-                    armed.arm(0, ic & 1);
-                    ++ic;
-#pragma unroll
-                    for (int s = 0; s < C::kSlabs; ++s) {
-                        tma_load_5d(sK + s * C::kSlab, &map_k, kv_full, 64 * s, c.u0, 0, c.hk, c.b);
-                        tma_load_5d(sV + s * C::kSlab, &map_v, kv_full, 64 * s, c.u0, 0, c.hk, c.b);
-                    }
-                    for (int i = 0; i < c.n; ++i, ++g) {
-                        const int st = g % C::kStages;
-                        const uint32_t par = (g / C::kStages) & 1;
-                        const int h = c.h0 + i / c.per_head, t0 = c.t_lo + kHalf * (i % c.per_head);
-                        ok = mbar_wait_abortable(q_free(st), par ^ 1, 0x211, abort_flag);
-                        if (!ok) break;
-                        mbar_expect_tx(q_full(st), 2 * C::kQTile + C::kStat);
-                        armed.arm(1 + st, par);
-#pragma unroll
-                        for (int s = 0; s < C::kSlabs; ++s) {
-                            tma_load_5d(sQ(st) + s * C::kQSlab, &map_q, q_full(st), 64 * s, t0, 0, h, c.b);
-                            tma_load_5d(sG(st) + s * C::kQSlab, &map_g, q_full(st), 64 * s, t0, 0, h, c.b);
+                    // (the first query rows of an item are requested while the last item's products still read its K and V)
+                    const int early = min(2, c.n);
+                    int h = c.h0, step = 0;
+                    for (int i = 0; i < c.n; ++i, q.next(), ++step) {
+                        if (step == c.per_head) {
+                            step = 0;
+                            ++h;
                         }
+                        const int t0 = c.t_lo + kHalf * step;
+                        ok = mbar_wait_abortable(q_free(q.st), q.ph ^ 1, 0x211, abort_flag);
+                        if (!ok) break;
+                        mbar_expect_tx(q_full(q.st), 2 * C::kQTile + C::kStat);
+                        armed.arm(1 + q.st, q.ph);
+                        tma_load_5d(sQ(q.st), &map_q, q_full(q.st), 0, t0, 0, h, c.b);
+                        tma_load_5d(sG(q.st), &map_g, q_full(q.st), 0, t0, 0, h, c.b);
                         // (the statistics are padded to whole tiles of rows)
-                        bulk_load(s0 + C::kOffStat + st * C::kStat, a.stats + (((long long)c.b * a.H + h) * a.prow + t0) * 4, C::kStat,
-                                  q_full(st));
+                        bulk_load(s0 + C::kOffStat + q.st * C::kStat, a.stats + (((long long)c.b * a.H + h) * a.prow + t0) * 4, C::kStat,
+                                  q_full(q.st));
+                        if (i + 1 == early) {
+                            ok = mbar_wait_abortable(kv_free, kph, 0x210, abort_flag);
+                            if (!ok) break;
+                            mbar_expect_tx(kv_full, 2 * C::kTile);
+                            armed.arm(0, kph ^ 1);
+                            kph ^= 1;
+                            tma_load_5d(sK, &map_k, kv_full, 0, c.u0, 0, c.hk, c.b);
+                            tma_load_5d(sV, &map_v, kv_full, 0, c.u0, 0, c.hk, c.b);
+                        }
                     }
                 }
                 if (!ok) armed.drain(bar0, 1 + C::kStages);
             }
         } else if (warp == 1) {
             // =========================================================== MMA issuer
-            constexpr uint32_t idesc_s = instr_desc(kHalf, 0);
-            constexpr uint32_t idesc_v = instr_desc(D, 1);
-            constexpr uint32_t idesc_k = instr_desc(C::kd, 1);
-            const uint32_t k_low = desc_low(sK, 16), v_low = desc_low(sV, 16);
-            uint32_t ic = 0, g0 = 0, sr[2] = {0, 0}, sd[2] = {0, 0};
-            bool ok = true;
-            auto scores = [&](const DkvItem &c, int i) {
-                const uint32_t g = g0 + (uint32_t)i;
-                const int st = g % C::kStages, ch = i & 1;
-                if (!warp_wait(q_full(st), (g / C::kStages) & 1, 0x220, abort_flag)) return false;
-                const int t0 = c.t_lo + kHalf * (i % c.per_head);
-                // rows the tensors have but the call does not count: they meet weights of 0 in the products for dK, dV
-                if (c.sp.ql < a.Nq && c.sp.ql < t0 + kHalf) {
-                    zero_rows(sQ(st), C::kQSlab, C::kSlabs, c.sp.ql - t0, kHalf);
-                    zero_rows(sG(st), C::kQSlab, C::kSlabs, c.sp.ql - t0, kHalf);
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                }
-                tc_fence_after();
-                const uint32_t ql = desc_low(sQ(st), 16), gl = desc_low(sG(st), 16), x = tmem_base + ch * 128, y = x + 64;
-                if (elect_one()) {
+            if (elect_one()) {
+                constexpr uint32_t idesc_s = instr_desc(kHalf, 0);
+                constexpr uint32_t idesc_v = instr_desc(D, 1);
+                constexpr uint32_t idesc_k = instr_desc(C::kd, 1);
+                const uint32_t k_low = desc_low(sK, 16), v_low = desc_low(sV, 16);
+                Ring<C::kStages> qa, qb, qc;         // stages of the next dA and S_1, the next S_2, the next dV and dK
+                uint32_t iph = 0, rpar = 0, dpar = 0;   // phase of the item; bit ch: phases of da_read, ds_full
+                bool ok = true, ql_cut = false;      // whether rows that do not count stand behind those that do
+                // dA and S_1 of the next step, whose first row is `left` rows before the end of those that count
+                auto scores = [&](int ch, int left) {
+                    if (!mbar_wait_abortable(q_full(qa.st), qa.ph, 0x220, abort_flag)) return false;
+                    // rows behind the end, up to the last step of 16 the products for dK, dV take, become rows of zeros: their
+                    // weights are then 2^(0 - inf) = 0
+                    if (left < kHalf && ql_cut) {
+                        zero_rows(sQ(qa.st), C::kQSlab, C::kSlabs, left, (left + 15) & ~15);
+                        zero_rows(sG(qa.st), C::kQSlab, C::kSlabs, left, (left + 15) & ~15);
+                        fence_proxy_async_smem();
+                    }
+                    tc_fence_after();
+                    const uint32_t ql = desc_low(sQ(qa.st), 16), gl = desc_low(sG(qa.st), 16), x = tmem_base + ch * 128, y = x + 64;
 #pragma unroll
                     for (int kb = 0; kb < D / 16; ++kb)
                         mma_ss(x, v_low + (((kb >> 2) * C::kSlab + (kb & 3) * 32) >> 4),
@@ -564,68 +520,78 @@ diff_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     for (int kb = 0; kb < C::kd / 16; ++kb)
                         mma_ss(y, k_low + (map_k_off<D>(0, kb, C::kSlab) >> 4), ql + (map_k_off<D>(0, kb, C::kQSlab) >> 4), idesc_s, kb > 0);
                     tc_commit(s_full(ch));
-                }
-                __syncwarp();
-                return true;
-            };
-            for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
-                const int item = item_of_round(a, round);
-                if (item < 0) continue;
-                const DkvItem c = decode_dkv(a, item);
-                if (c.n == 0) continue;
-                ok = warp_wait(kv_full, ic & 1, 0x221, abort_flag);
-                if (ok) ok = scores(c, 0);
-                if (ok && c.n > 1) ok = scores(c, 1);
-                for (int i = 0; ok && i <= c.n; ++i) {
-                    if (i < c.n) {
-                        // S_2 of step i, once its dA is in registers
-                        const int ch = i & 1, st = (g0 + (uint32_t)i) % C::kStages;
-                        ok = warp_wait(da_read(ch), sr[ch] & 1, 0x222, abort_flag);
-                        ++sr[ch];
-                        if (!ok) break;
-                        tc_fence_after();
-                        const uint32_t ql = desc_low(sQ(st), 16), x = tmem_base + ch * 128;
-                        if (elect_one()) {
+                    qa.next();
+                    return true;
+                };
+                for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
+                    const int item = item_of_round(a.total_items, round);
+                    if (item < 0) continue;
+                    const DkvItem c = decode_dkv(a, item);
+                    if (c.n == 0) continue;
+                    // rows from the head's first step to the end, less those before the next scores / the next dV, dK
+                    const int all = c.sp.ql - c.t_lo;
+                    int left_s = all, left = all;
+                    auto next_scores = [&](int ch) {
+                        const bool fine = scores(ch, left_s);
+                        left_s -= kHalf;
+                        if (left_s <= 0) left_s = all;
+                        return fine;
+                    };
+                    ql_cut = c.sp.ql < a.Nq;
+                    ok = mbar_wait_abortable(kv_full, iph, 0x221, abort_flag);
+                    if (ok) ok = next_scores(0);
+                    if (ok && c.n > 1) ok = next_scores(1);
+                    for (int i = 0; ok && i <= c.n; ++i) {
+                        if (i < c.n) {
+                            // S_2 of step i, once its dA is in registers
+                            const int ch = i & 1;
+                            ok = mbar_wait_abortable(da_read(ch), (rpar >> ch) & 1, 0x222, abort_flag);
+                            rpar ^= 1u << ch;
+                            if (!ok) break;
+                            tc_fence_after();
+                            const uint32_t ql = desc_low(sQ(qb.st), 16), x = tmem_base + ch * 128;
 #pragma unroll
                             for (int kb = 0; kb < C::kd / 16; ++kb)
                                 mma_ss(x, k_low + (map_k_off<D>(1, kb, C::kSlab) >> 4), ql + (map_k_off<D>(1, kb, C::kQSlab) >> 4),
                                        idesc_s, kb > 0);
                             tc_commit(s2_full(ch));
+                            qb.next();
                             if (i + 1 == c.n) tc_commit(kv_free);
                         }
-                        __syncwarp();
-                    }
-                    if (i >= 1) {
-                        // dV, dK of step i - 1, then dA and S_1 of step i + 1 in the same slots
-                        const int k = i - 1, ch = k & 1, st = (g0 + (uint32_t)k) % C::kStages;
-                        ok = warp_wait(ds_full(ch), sd[ch] & 1, 0x223, abort_flag);
-                        ++sd[ch];
-                        if (ok && k == 0) ok = warp_wait(acc_free, (ic & 1) ^ 1, 0x224, abort_flag);
-                        if (!ok) break;
-                        tc_fence_after();
-                        const uint32_t x = tmem_base + ch * 128, y = x + 64, first = k > 0 ? 1u : 0u;
-                        const uint32_t gl = desc_low(sG(st), C::kQSlab), ql = desc_low(sQ(st), C::kQSlab);
-                        if (elect_one()) {
+                        if (i >= 1) {
+                            // dV, dK of step i - 1, then dA and S_1 of step i + 1 in the same slots
+                            const int ch = (i - 1) & 1;
+                            ok = mbar_wait_abortable(ds_full(ch), (dpar >> ch) & 1, 0x223, abort_flag);
+                            dpar ^= 1u << ch;
+                            if (ok && i == 1) ok = mbar_wait_abortable(acc_free, iph ^ 1, 0x224, abort_flag);
+                            if (!ok) break;
+                            const int ksteps = min(kHalf / 16, (left + 15) >> 4);
+                            left -= kHalf;
+                            if (left <= 0) left = all;
+                            tc_fence_after();
+                            const uint32_t x = tmem_base + ch * 128, y = x + 64, first = i > 1 ? 1u : 0u;
+                            const uint32_t gl = desc_low(sG(qc.st), C::kQSlab), ql = desc_low(sQ(qc.st), C::kQSlab);
 #pragma unroll
                             for (int kb = 0; kb < kHalf / 16; ++kb)
-                                mma_ts(tmem_base + C::kColDV, y + 16 * kb, gl + 128u * kb, idesc_v, kb > 0 ? 1u : first);
+                                if (kb < ksteps) mma_ts(tmem_base + C::kColDV, y + 16 * kb, gl + 128u * kb, idesc_v, kb > 0 ? 1u : first);
 #pragma unroll
                             for (int kb = 0; kb < kHalf / 16; ++kb)
-                                mma_ts(tmem_base + C::kColDK, y + 16 * kb + 8, ql + (map_n_off<D>(0, C::kQSlab) >> 4) + 128u * kb,
-                                       idesc_k, kb > 0 ? 1u : first);
+                                if (kb < ksteps)
+                                    mma_ts(tmem_base + C::kColDK, y + 16 * kb + 8, ql + (map_n_off<D>(0, C::kQSlab) >> 4) + 128u * kb, idesc_k,
+                                           kb > 0 ? 1u : first);
 #pragma unroll
                             for (int kb = 0; kb < kHalf / 16; ++kb)
-                                mma_ts(tmem_base + C::kColDK + C::kd, x + 16 * kb,
-                                       ql + (map_n_off<D>(1, C::kQSlab) >> 4) + 128u * kb, idesc_k, kb > 0 ? 1u : first);
-                            tc_commit(q_free(st));
+                                if (kb < ksteps)
+                                    mma_ts(tmem_base + C::kColDK + C::kd, x + 16 * kb, ql + (map_n_off<D>(1, C::kQSlab) >> 4) + 128u * kb,
+                                           idesc_k, kb > 0 ? 1u : first);
+                            tc_commit(q_free(qc.st));
+                            qc.next();
                             if (i == c.n) tc_commit(acc_full);
+                            if (i + 1 < c.n) ok = next_scores(ch);
                         }
-                        __syncwarp();
-                        if (i + 1 < c.n) ok = scores(c, i + 1);
                     }
+                    iph ^= 1u;
                 }
-                g0 += (uint32_t)c.n;
-                ++ic;
             }
         }
     } else {
@@ -637,7 +603,7 @@ diff_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         bool ok = true;
         uint32_t ic = 0, g = ch, sc = 0;             // g: steps of both chains, this chain's next
         for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
-            const int item = item_of_round(a, round);
+            const int item = item_of_round(a.total_items, round);
             if (item < 0) continue;
             // (few numbers are kept over the steps; the epilogue works the item out again)
             int n, per_head, h, cl;                  // cl: columns of the chain's first step that do not see this key
@@ -801,7 +767,7 @@ diff_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 
 template <int D>
 int launch_d(const DiffProblem &p, const DiffGrads &g) {
-    CUtensorMap mq, mg, mk, mv, mqh, mgh;
+    CUtensorMap mq, mg, mk, mv, mqh, mgh, mkh, mvh;
     int rc;
     if ((rc = make_strided_map(&mq, p.q, &p.sq.b, p.B, p.H, p.Nq, D, kRows)) != TA_OK) return rc;
     if ((rc = make_strided_map(&mg, p.dout, &p.sdo.b, p.B, p.H, p.Nq, D, kRows)) != TA_OK) return rc;
@@ -809,6 +775,8 @@ int launch_d(const DiffProblem &p, const DiffGrads &g) {
     if ((rc = make_strided_map(&mv, p.v, &p.sv.b, p.B, p.H_kv, p.Nk, D, kRows)) != TA_OK) return rc;
     if ((rc = make_strided_map(&mqh, p.q, &p.sq.b, p.B, p.H, p.Nq, D, kHalf)) != TA_OK) return rc;
     if ((rc = make_strided_map(&mgh, p.dout, &p.sdo.b, p.B, p.H, p.Nq, D, kHalf)) != TA_OK) return rc;
+    if ((rc = make_strided_map(&mkh, p.k, &p.sk.b, p.B, p.H_kv, p.Nk, D, kHalf)) != TA_OK) return rc;
+    if ((rc = make_strided_map(&mvh, p.v, &p.sv.b, p.B, p.H_kv, p.Nk, D, kHalf)) != TA_OK) return rc;
     int dev = 0;
     const int num_sms = current_device_sms(&dev);
     static PerDeviceOnce configured;
@@ -840,7 +808,7 @@ int launch_d(const DiffProblem &p, const DiffGrads &g) {
     a.total_items = (int)dq_items;
     a.tile_major = 2ull * p.B * p.H_kv * p.Nk * D * 2 <= (96ull << 20) ? 1 : 0;
     rc = launch_kernel(diff_tc_dq_kernel<D>, (unsigned)(a.total_items < num_sms ? a.total_items : num_sms), kThreads,
-                       DqCfg<D>::kSmem, p.stream, false, mq, mg, mk, mv, a);
+                       DqCfg<D>::kSmem, p.stream, false, mq, mg, mkh, mvh, a);
     if (rc != TA_OK) return rc;
     a.tiles = (p.Nk + kRows - 1) / kRows;
     a.total_items = (int)dkv_items;

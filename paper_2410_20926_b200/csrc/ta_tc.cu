@@ -554,8 +554,9 @@ int make_view_map(CUtensorMap *map, const void *base, int heads_total, int N, in
     return TA_OK;
 }
 
-// Rank-5 map (D, token, 1, head, batch) of a strided bf16 tensor [B][heads][N][D]; strides in elements (batch, head, token),
-// multiples of 8; box: 64 features of `box_rows` tokens of one head, 128-byte swizzle.
+// Rank-5 map (64 features, token, D / 64, head, batch) of a strided bf16 tensor [B][heads][N][D]; strides in elements (batch,
+// head, token), multiples of 8; box: all features of `box_rows` tokens of one head, landing as D / 64 slabs of 128-byte
+// rows (128-byte swizzle): one copy per tile, since the issuing thread needs about 150 cycles for each.
 int make_strided_map(CUtensorMap *map, const void *base, const long long *strides, int B, int heads, int N, int D, int box_rows) {
     EncodeTiledFn enc = encode_fn();
     if (!enc) {
@@ -566,9 +567,9 @@ int make_strided_map(CUtensorMap *map, const void *base, const long long *stride
     const cuuint64_t row = N > 1 ? (cuuint64_t)strides[2] * 2 : (cuuint64_t)D * 2;
     const cuuint64_t head = heads > 1 ? (cuuint64_t)strides[1] * 2 : row;
     const cuuint64_t batch = B > 1 ? (cuuint64_t)strides[0] * 2 : row;
-    cuuint64_t gdim[5] = {(cuuint64_t)D, (cuuint64_t)N, 1, (cuuint64_t)heads, (cuuint64_t)B};
-    cuuint64_t gstr[4] = {row, row, head, batch};
-    cuuint32_t box[5] = {64u, (cuuint32_t)box_rows, 1u, 1u, 1u};
+    cuuint64_t gdim[5] = {64, (cuuint64_t)N, (cuuint64_t)(D / 64), (cuuint64_t)heads, (cuuint64_t)B};
+    cuuint64_t gstr[4] = {row, 128, head, batch};
+    cuuint32_t box[5] = {64u, (cuuint32_t)box_rows, (cuuint32_t)(D / 64), 1u, 1u};
     cuuint32_t estr[5] = {1, 1, 1, 1, 1};
     if (!thread_has_context()) cudaFree(nullptr);   // (see make_view_map)
     auto encode = [&] {
