@@ -12,9 +12,10 @@
 // Tensor memory: two score slots of 64 columns per chain, so that a chain's next scores are formed while it works on
 // these, and O_1, O_2 -- 512 columns at head dim 128.
 //
-// One CTA per SM, persistent: warp 0 loads (TMA), warp 1 issues the MMAs in a fixed order -- P V of half block h, then S of
-// half block h + 2 into the slot this frees, chain after chain --, warps 4-7 and 8-11 are the softmax of chain 1 and 2
-// (one query row per thread).  A quarter of the exponentials are polynomials on the multiply-add pipes (exp2_poly).  A
+// One CTA per SM, persistent: warp 0 loads (TMA), one thread of warp 1 issues the MMAs in a fixed order -- P V of half block
+// h, then S of half block h + 2 into the slots this frees, both chains each time --, warps 4-7 and 8-11 are the softmax
+// of chain 1 and 2 (one query row per thread).  The issuing thread's own instructions, above all its waits (about 100
+// cycles each) and commits, have to fit beside the products: it waits twice and commits three times per half block.  A quarter of the exponentials are polynomials on the multiply-add pipes (exp2_poly).  A
 // running maximum is moved (and O rescaled) only when it has grown by more than 2^8: weights up to 256 lose nothing in
 // bf16 or fp32.  Every wait is bounded; when one expires the CTA raises a flag that ends all roles, lets its copies land,
 // frees its tensor memory and returns.
@@ -37,12 +38,12 @@ struct Cfg {
     static constexpr int kd = D / 2;
     static constexpr uint32_t kTile = kSlabs * kSlab, kHTile = kSlabs * kHSlab;
     static constexpr int kNQ = 2;
-    static constexpr int kNKV = 5;                 // stages of 64 keys, K and V apart
+    static constexpr int kNKV = 5;                 // stages of 64 keys
     static constexpr uint32_t kOffQ = 0;
     static constexpr uint32_t kOffK = kOffQ + kNQ * kTile;
     static constexpr uint32_t kOffV = kOffK + kNKV * kHTile;
     static constexpr uint32_t kOffBar = kOffV + kNKV * kHTile;
-    static constexpr int kNumBars = 2 * kNQ + 4 * kNKV + 4 + 4 + 2 + 2 + 2;
+    static constexpr int kNumBars = 2 * kNQ + 2 * kNKV + 2 + 2 + 4;
     static constexpr uint32_t kOffX = kOffBar + ((kNumBars * 8 + 16 + 15) & ~15);      // 1 / l of both maps, 128 rows
     static constexpr uint32_t kSmem = kOffX + 2 * kRows * 4 + 1024;
     static constexpr uint32_t kColO = 256;
@@ -105,21 +106,19 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     auto sV = [&](int i) { return s0 + C::kOffV + (uint32_t)i * C::kHTile; };
     const uint32_t bar0 = s0 + C::kOffBar;
     auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
-    // barriers 0 .. kNQ + 2 kNKV - 1 are those copies complete on
+    // barriers 0 .. kNQ + kNKV - 1 are those copies complete on
     auto q_full = [&](int i) { return bar(i); };
-    auto k_full = [&](int i) { return bar(C::kNQ + i); };
-    auto v_full = [&](int i) { return bar(C::kNQ + C::kNKV + i); };
-    constexpr int kA = C::kNQ + 2 * C::kNKV;
+    auto kv_full = [&](int i) { return bar(C::kNQ + i); };
+    constexpr int kA = C::kNQ + C::kNKV;
     auto q_free = [&](int i) { return bar(kA + i); };
-    auto k_free = [&](int i) { return bar(kA + C::kNQ + i); };
-    auto v_free = [&](int i) { return bar(kA + C::kNQ + C::kNKV + i); };
-    constexpr int kB = 2 * C::kNQ + 4 * C::kNKV;
-    auto s_full = [&](int c, int p) { return bar(kB + 2 * c + p); };       // scores of chain c in slot p complete
-    auto p_full = [&](int c, int p) { return bar(kB + 4 + 2 * c + p); };   // weights of chain c in slot p written (4 warps)
-    auto pv_done = [&](int c) { return bar(kB + 8 + c); };                 // a value product of chain c complete
-    auto o_full = [&](int c) { return bar(kB + 10 + c); };                 // value sum of chain c complete
-    const uint32_t o_free = bar(kB + 12);                                  // both value sums read (8 warps)
-    const uint32_t x_full = bar(kB + 13);                                  // 1 / l of both maps written (8 warps)
+    auto kv_free = [&](int i) { return bar(kA + C::kNQ + i); };
+    constexpr int kB = 2 * C::kNQ + 2 * C::kNKV;
+    auto s_full = [&](int p) { return bar(kB + p); };           // scores of both chains in slot p complete
+    auto p_full = [&](int p) { return bar(kB + 2 + p); };       // weights of both chains in slot p written (8 warps)
+    const uint32_t pv_done = bar(kB + 4);                       // value products of a half block complete
+    const uint32_t o_full = bar(kB + 5);                        // value sums complete
+    const uint32_t o_free = bar(kB + 6);                        // and read (8 warps)
+    const uint32_t x_full = bar(kB + 7);                        // 1 / l of both maps written (8 warps)
     uint32_t *tmem_slot = (uint32_t *)(smem + C::kOffBar + C::kNumBars * 8);
     volatile uint32_t *abort_flag = tmem_slot + 1;
     float *s_inv = (float *)(smem + C::kOffX);
@@ -128,7 +127,7 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     // rows a tensor does not have arrive as zeros (TMA fill); nothing reads shared memory before it is loaded
     if (tid == 0) {
         for (int i = 0; i < C::kNumBars; ++i)
-            mbar_init(bar(i), i >= kB + 4 && i < kB + 8 ? 4 : i >= kB + 12 ? 8 : 1);
+            mbar_init(bar(i), i == kB + 2 || i == kB + 3 || i >= kB + 6 ? 8 : 1);
         *abort_flag = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -162,16 +161,12 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 tma_load_5d(sQ(q.st), &map_q, q_full(q.st), 0, c.t0, 0, c.h, c.b);
                 q.next();
                 for (int j = 0; j < c.n; ++j, kv.next()) {
-                    ok = mbar_wait_abortable(k_free(kv.st), kv.ph ^ 1, 0xD11, abort_flag);
+                    ok = mbar_wait_abortable(kv_free(kv.st), kv.ph ^ 1, 0xD11, abort_flag);
                     if (!ok) break;
-                    mbar_expect_tx(k_full(kv.st), C::kHTile);
+                    mbar_expect_tx(kv_full(kv.st), 2 * C::kHTile);
                     armed.arm(C::kNQ + kv.st, kv.ph);
-                    tma_load_5d(sK(kv.st), &map_k, k_full(kv.st), 0, kHalf * j, 0, c.hk, c.b);
-                    ok = mbar_wait_abortable(v_free(kv.st), kv.ph ^ 1, 0xD12, abort_flag);
-                    if (!ok) break;
-                    mbar_expect_tx(v_full(kv.st), C::kHTile);
-                    armed.arm(C::kNQ + C::kNKV + kv.st, kv.ph);
-                    tma_load_5d(sV(kv.st), &map_v, v_full(kv.st), 0, kHalf * j, 0, c.hk, c.b);
+                    tma_load_5d(sK(kv.st), &map_k, kv_full(kv.st), 0, kHalf * j, 0, c.hk, c.b);
+                    tma_load_5d(sV(kv.st), &map_v, kv_full(kv.st), 0, kHalf * j, 0, c.hk, c.b);
                 }
             }
             if (!ok) armed.drain(bar0, kA);
@@ -182,7 +177,7 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             constexpr uint32_t idesc_s = instr_desc(kHalf, 0);
             constexpr uint32_t idesc_o = instr_desc(D, 1);
             Ring<C::kNQ> q;
-            Ring<C::kNKV> k, v;
+            Ring<C::kNKV> k, v;                      // stage of the next scores, of the next value products
             uint32_t par = 0, oph = 1;               // bit p: phase of the weights in slot p; phase of o_free to wait for
             bool ok = true;
             for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
@@ -191,62 +186,61 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 const Item c = decode(a, item);
                 if (c.n == 0) continue;
                 const uint32_t q_low = desc_low(sQ(q.st), 16);
-                // scores of the half block in K's stage, chain ch, into slot p
-                auto scores = [&](int ch, int p, uint32_t k_low) {
+                // scores of the next half block, both chains, into slot p
+                auto scores = [&](int p) {
+                    if (!mbar_wait_abortable(kv_full(k.st), k.ph, 0xE11, abort_flag)) return false;
+                    const uint32_t k_low = desc_low(sK(k.st), 16), s = tmem_base + p * 64;
+                    tc_fence_after();
 #pragma unroll
-                    for (int kb = 0; kb < C::kd / 16; ++kb)
-                        mma_ss(tmem_base + ch * 128 + p * 64, q_low + map_k_off<D>(ch, kb, kSlab) / 16,
-                               k_low + map_k_off<D>(ch, kb, kHSlab) / 16, idesc_s, kb > 0);
-                    tc_commit(s_full(ch, p));
+                    for (int ch = 0; ch < 2; ++ch)
+#pragma unroll
+                        for (int kb = 0; kb < C::kd / 16; ++kb)
+                            mma_ss(s + ch * 128, q_low + map_k_off<D>(ch, kb, kSlab) / 16, k_low + map_k_off<D>(ch, kb, kHSlab) / 16, idesc_s,
+                                   kb > 0);
+                    tc_commit(s_full(p));
+                    k.next();
+                    return true;
                 };
                 ok = mbar_wait_abortable(q_full(q.st), q.ph, 0xE10, abort_flag);
-                for (int j = 0; ok && j < 2 && j < c.n; ++j) {
-                    ok = mbar_wait_abortable(k_full(k.st), k.ph, 0xE11, abort_flag);
-                    if (!ok) break;
-                    tc_fence_after();
-                    scores(0, j, desc_low(sK(k.st), 16));
-                    scores(1, j, desc_low(sK(k.st), 16));
-                    tc_commit(k_free(k.st));
-                    k.next();
-                }
-                for (int j = 0; ok && j < c.n; ++j) {
+                if (ok) ok = scores(0);
+                if (ok && c.n > 1) ok = scores(1);
+                if (ok) ok = mbar_wait_abortable(o_free, oph, 0xE15, abort_flag);
+                for (int j = 0; ok && j < c.n; ++j, v.next()) {
                     const int p = j & 1;
-                    const bool more = j + 2 < c.n;
-                    ok = mbar_wait_abortable(v_full(v.st), v.ph, 0xE12, abort_flag);
-                    if (ok && more) ok = mbar_wait_abortable(k_full(k.st), k.ph, 0xE13, abort_flag);
+                    ok = mbar_wait_abortable(p_full(p), (par >> p) & 1, 0xE14, abort_flag);
                     if (!ok) break;
-                    const int ksteps = min(kHalf / 16, (c.keys_end - kHalf * j + 15) >> 4);
-                    if (c.sp.kl < a.Nk && c.sp.kl < kHalf * j + 16 * ksteps) {
-                        zero_rows(sV(v.st), kHSlab, C::kSlabs, c.sp.kl - kHalf * j, 16 * ksteps);
-                        fence_proxy_async_smem();
-                    }
-                    const uint32_t v_low = desc_low(sV(v.st), kHSlab), k_low = desc_low(sK(k.st), 16), first = j > 0 ? 1u : 0u;
-#pragma unroll
-                    for (int ch = 0; ch < 2; ++ch) {
-                        ok = mbar_wait_abortable(p_full(ch, p), (par >> p) & 1, 0xE14, abort_flag);
-                        if (ok && j == 0 && ch == 0) ok = mbar_wait_abortable(o_free, oph, 0xE15, abort_flag);
-                        if (!ok) break;
-                        tc_fence_after();
-                        const uint32_t w = tmem_base + ch * 128 + p * 64;
-                        // (weights beyond ksteps are zeros that nothing has to multiply)
-#pragma unroll
-                        for (int kb = 0; kb < kHalf / 16; ++kb)
-                            if (kb < ksteps) mma_ts(tmem_base + C::kColO + ch * 128, w + kb * 8, v_low + 128u * kb, idesc_o, kb > 0 ? 1u : first);
-                        tc_commit(pv_done(ch));
-                        if (j + 1 == c.n) tc_commit(o_full(ch));
-                        if (ch == 1) tc_commit(v_free(v.st));
-                        if (more) scores(ch, p, k_low);
-                    }
-                    if (!ok) break;
-                    v.next();
-                    if (more) {
-                        tc_commit(k_free(k.st));
-                        k.next();
-                    }
                     par ^= 1u << p;
+                    const uint32_t v_low = desc_low(sV(v.st), kHSlab), w = tmem_base + p * 64, o = tmem_base + C::kColO;
+                    const uint32_t first = j > 0 ? 1u : 0u;
+                    if (j + 1 < c.n) {
+                        tc_fence_after();
+#pragma unroll
+                        for (int ch = 0; ch < 2; ++ch)
+#pragma unroll
+                            for (int kb = 0; kb < kHalf / 16; ++kb)
+                                mma_ts(o + ch * 128, w + ch * 128 + kb * 8, v_low + 128u * kb, idesc_o, kb > 0 ? 1u : first);
+                        tc_commit(pv_done);
+                        tc_commit(kv_free(v.st));
+                        if (j + 2 < c.n) ok = scores(p);
+                    } else {
+                        // the last half block: only the steps of 16 keys that hold some (the weights beyond them are zeros)
+                        const int ksteps = (c.keys_end - kHalf * j + 15) >> 4;
+                        if (c.sp.kl < a.Nk && c.sp.kl < kHalf * j + 16 * ksteps) {
+                            zero_rows(sV(v.st), kHSlab, C::kSlabs, c.sp.kl - kHalf * j, 16 * ksteps);
+                            fence_proxy_async_smem();
+                        }
+                        tc_fence_after();
+#pragma unroll 1
+                        for (int ch = 0; ch < 2; ++ch)
+#pragma unroll 1
+                            for (int kb = 0; kb < ksteps; ++kb)
+                                mma_ts(o + ch * 128, w + ch * 128 + kb * 8, v_low + 128u * kb, idesc_o, kb > 0 ? 1u : first);
+                        tc_commit(pv_done);
+                        tc_commit(kv_free(v.st));
+                        tc_commit(o_full);
+                        tc_commit(q_free(q.st));
+                    }
                 }
-                // every score of the item has been issued
-                tc_commit(q_free(q.st));
                 q.next();
                 oph ^= 1u;
             }
@@ -271,7 +265,7 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             for (int j = 0; j < c.n; ++j, ++sc) {
                 const int p = j & 1;
                 const uint32_t col = s_col + 64 * p;
-                ok = warp_wait(s_full(ch, p), (par >> p) & 1, 0xF10, abort_flag);
+                ok = warp_wait(s_full(p), (par >> p) & 1, 0xF10, abort_flag);
                 par ^= 1u << p;
                 if (!ok) break;
                 tc_fence_after();
@@ -303,7 +297,7 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                     if (j > 0) {
                         // (the scores of this half block were issued behind the value product before the last: only the last
                         // one's phase can be open)
-                        ok = warp_wait(pv_done(ch), (sc - 1) & 1, 0xF14, abort_flag);
+                        ok = warp_wait(pv_done, (sc - 1) & 1, 0xF14, abort_flag);
                         if (!ok) break;
                         tc_fence_after();
 #pragma unroll 1
@@ -332,7 +326,7 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_full(ch, p));
+                if (lane == 0) mbar_arrive(p_full(p));
             }
             if (!ok) break;
 
@@ -347,8 +341,7 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 __syncwarp();
                 if (lane == 0) mbar_arrive(x_full);
                 ok = warp_wait(x_full, ic & 1, 0xF13, abort_flag);
-                if (ok) ok = warp_wait(o_full(0), ic & 1, 0xF11, abort_flag);
-                if (ok) ok = warp_wait(o_full(1), ic & 1, 0xF12, abort_flag);
+                if (ok) ok = warp_wait(o_full, ic & 1, 0xF11, abort_flag);
                 ++ic;
                 i1 = s_inv[r];
                 i2 = s_inv[kRows + r] * lam;
