@@ -13,9 +13,10 @@
 // these, and O_1, O_2 -- 512 columns at head dim 128.
 //
 // One CTA per SM, persistent: warp 0 loads (TMA), one thread of warp 1 issues the MMAs in a fixed order -- P V of half block
-// h, then S of half block h + 2 into the slots this frees, both chains each time --, warps 4-7 and 8-11 are the softmax
-// of chain 1 and 2 (one query row per thread).  The issuing thread's own instructions, above all its waits (about 100
-// cycles each) and commits, have to fit beside the products: it waits twice and commits three times per half block.  A quarter of the exponentials are polynomials on the multiply-add pipes (exp2_poly).  A
+// h, then S of half block h + 2 into the slot this frees, chain after chain --, warps 4-7 and 8-11 are the softmax of
+// chain 1 and 2 (one query row per thread).  The chains run half a step apart, so that one is at its maxima while the
+// other keeps the special-function units busy (in step they were 15 % slower).  The issuing thread's own instructions,
+// above all its waits (about 100 cycles each) and commits, have to fit beside the products.  An eighth of the exponentials are polynomials on the multiply-add pipes (exp2_poly).  A
 // running maximum is moved (and O rescaled) only when it has grown by more than 2^8: weights up to 256 lose nothing in
 // bf16 or fp32.  Every wait is bounded; when one expires the CTA raises a flag that ends all roles, lets its copies land,
 // frees its tensor memory and returns.
@@ -43,7 +44,7 @@ struct Cfg {
     static constexpr uint32_t kOffK = kOffQ + kNQ * kTile;
     static constexpr uint32_t kOffV = kOffK + kNKV * kHTile;
     static constexpr uint32_t kOffBar = kOffV + kNKV * kHTile;
-    static constexpr int kNumBars = 2 * kNQ + 2 * kNKV + 2 + 2 + 4;
+    static constexpr int kNumBars = 2 * kNQ + 2 * kNKV + 4 + 4 + 2 + 3;
     static constexpr uint32_t kOffX = kOffBar + ((kNumBars * 8 + 16 + 15) & ~15);      // 1 / l of both maps, 128 rows
     static constexpr uint32_t kSmem = kOffX + 2 * kRows * 4 + 1024;
     static constexpr uint32_t kColO = 256;
@@ -113,12 +114,12 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     auto q_free = [&](int i) { return bar(kA + i); };
     auto kv_free = [&](int i) { return bar(kA + C::kNQ + i); };
     constexpr int kB = 2 * C::kNQ + 2 * C::kNKV;
-    auto s_full = [&](int p) { return bar(kB + p); };           // scores of both chains in slot p complete
-    auto p_full = [&](int p) { return bar(kB + 2 + p); };       // weights of both chains in slot p written (8 warps)
-    const uint32_t pv_done = bar(kB + 4);                       // value products of a half block complete
-    const uint32_t o_full = bar(kB + 5);                        // value sums complete
-    const uint32_t o_free = bar(kB + 6);                        // and read (8 warps)
-    const uint32_t x_full = bar(kB + 7);                        // 1 / l of both maps written (8 warps)
+    auto s_full = [&](int c, int p) { return bar(kB + 2 * c + p); };       // scores of chain c in slot p complete
+    auto p_full = [&](int c, int p) { return bar(kB + 4 + 2 * c + p); };   // weights of chain c in slot p written (4 warps)
+    auto pv_done = [&](int c) { return bar(kB + 8 + c); };                 // value product of a half block complete
+    const uint32_t o_full = bar(kB + 10);                                  // value sums complete
+    const uint32_t o_free = bar(kB + 11);                                  // and read (8 warps)
+    const uint32_t x_full = bar(kB + 12);                                  // 1 / l of both maps written (8 warps)
     uint32_t *tmem_slot = (uint32_t *)(smem + C::kOffBar + C::kNumBars * 8);
     volatile uint32_t *abort_flag = tmem_slot + 1;
     float *s_inv = (float *)(smem + C::kOffX);
@@ -127,7 +128,7 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     // rows a tensor does not have arrive as zeros (TMA fill); nothing reads shared memory before it is loaded
     if (tid == 0) {
         for (int i = 0; i < C::kNumBars; ++i)
-            mbar_init(bar(i), i == kB + 2 || i == kB + 3 || i >= kB + 6 ? 8 : 1);
+            mbar_init(bar(i), i >= kB + 4 && i < kB + 8 ? 4 : i >= kB + 11 ? 8 : 1);
         *abort_flag = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -154,14 +155,14 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 if (item < 0) continue;
                 const Item c = decode(a, item);
                 if (c.n == 0) continue;
-                ok = mbar_wait_abortable(q_free(q.st), q.ph ^ 1, 0xD10, abort_flag);
+                ok = sleep_wait(q_free(q.st), q.ph ^ 1, 0xD10, abort_flag);
                 if (!ok) break;
                 mbar_expect_tx(q_full(q.st), C::kTile);
                 armed.arm(q.st, q.ph);
                 tma_load_5d(sQ(q.st), &map_q, q_full(q.st), 0, c.t0, 0, c.h, c.b);
                 q.next();
                 for (int j = 0; j < c.n; ++j, kv.next()) {
-                    ok = mbar_wait_abortable(kv_free(kv.st), kv.ph ^ 1, 0xD11, abort_flag);
+                    ok = sleep_wait(kv_free(kv.st), kv.ph ^ 1, 0xD11, abort_flag);
                     if (!ok) break;
                     mbar_expect_tx(kv_full(kv.st), 2 * C::kHTile);
                     armed.arm(C::kNQ + kv.st, kv.ph);
@@ -186,42 +187,47 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 const Item c = decode(a, item);
                 if (c.n == 0) continue;
                 const uint32_t q_low = desc_low(sQ(q.st), 16);
-                // scores of the next half block, both chains, into slot p
-                auto scores = [&](int p) {
-                    if (!mbar_wait_abortable(kv_full(k.st), k.ph, 0xE11, abort_flag)) return false;
-                    const uint32_t k_low = desc_low(sK(k.st), 16), s = tmem_base + p * 64;
-                    tc_fence_after();
+                // scores of the half block whose K starts at k_low, chain ch, into slot p
+                auto scores = [&](int ch, int p, uint32_t k_low) {
 #pragma unroll
-                    for (int ch = 0; ch < 2; ++ch)
-#pragma unroll
-                        for (int kb = 0; kb < C::kd / 16; ++kb)
-                            mma_ss(s + ch * 128, q_low + map_k_off<D>(ch, kb, kSlab) / 16, k_low + map_k_off<D>(ch, kb, kHSlab) / 16, idesc_s,
-                                   kb > 0);
-                    tc_commit(s_full(p));
-                    k.next();
-                    return true;
+                    for (int kb = 0; kb < C::kd / 16; ++kb)
+                        mma_ss(tmem_base + ch * 128 + p * 64, q_low + map_k_off<D>(ch, kb, kSlab) / 16,
+                               k_low + map_k_off<D>(ch, kb, kHSlab) / 16, idesc_s, kb > 0);
+                    tc_commit(s_full(ch, p));
                 };
-                ok = mbar_wait_abortable(q_full(q.st), q.ph, 0xE10, abort_flag);
-                if (ok) ok = scores(0);
-                if (ok && c.n > 1) ok = scores(1);
-                if (ok) ok = mbar_wait_abortable(o_free, oph, 0xE15, abort_flag);
+                ok = sleep_wait(q_full(q.st), q.ph, 0xE10, abort_flag);
+                for (int j = 0; ok && j < 2 && j < c.n; ++j, k.next()) {
+                    ok = sleep_wait(kv_full(k.st), k.ph, 0xE11, abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                    scores(0, j, desc_low(sK(k.st), 16));
+                    scores(1, j, desc_low(sK(k.st), 16));
+                }
+                if (ok) ok = sleep_wait(o_free, oph, 0xE15, abort_flag);
                 for (int j = 0; ok && j < c.n; ++j, v.next()) {
                     const int p = j & 1;
-                    ok = mbar_wait_abortable(p_full(p), (par >> p) & 1, 0xE14, abort_flag);
-                    if (!ok) break;
+                    const bool more = j + 2 < c.n;
+                    const uint32_t ph = (par >> p) & 1;
                     par ^= 1u << p;
                     const uint32_t v_low = desc_low(sV(v.st), kHSlab), w = tmem_base + p * 64, o = tmem_base + C::kColO;
                     const uint32_t first = j > 0 ? 1u : 0u;
                     if (j + 1 < c.n) {
-                        tc_fence_after();
+                        const uint32_t k_low = desc_low(sK(k.st), 16);
+                        if (more) ok = sleep_wait(kv_full(k.st), k.ph, 0xE12, abort_flag);
+                        if (!ok) break;
 #pragma unroll
-                        for (int ch = 0; ch < 2; ++ch)
+                        for (int ch = 0; ch < 2; ++ch) {
+                            ok = sleep_wait(p_full(ch, p), ph, 0xE14, abort_flag);
+                            if (!ok) break;
+                            tc_fence_after();
 #pragma unroll
                             for (int kb = 0; kb < kHalf / 16; ++kb)
                                 mma_ts(o + ch * 128, w + ch * 128 + kb * 8, v_low + 128u * kb, idesc_o, kb > 0 ? 1u : first);
-                        tc_commit(pv_done);
-                        tc_commit(kv_free(v.st));
-                        if (j + 2 < c.n) ok = scores(p);
+                            tc_commit(pv_done(ch));
+                            if (ch == 1) tc_commit(kv_free(v.st));
+                            if (more) scores(ch, p, k_low);
+                        }
+                        if (more) k.next();
                     } else {
                         // the last half block: only the steps of 16 keys that hold some (the weights beyond them are zeros)
                         const int ksteps = (c.keys_end - kHalf * j + 15) >> 4;
@@ -229,13 +235,16 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                             zero_rows(sV(v.st), kHSlab, C::kSlabs, c.sp.kl - kHalf * j, 16 * ksteps);
                             fence_proxy_async_smem();
                         }
-                        tc_fence_after();
 #pragma unroll 1
-                        for (int ch = 0; ch < 2; ++ch)
+                        for (int ch = 0; ch < 2; ++ch) {
+                            ok = sleep_wait(p_full(ch, p), ph, 0xE16, abort_flag);
+                            if (!ok) break;
+                            tc_fence_after();
 #pragma unroll 1
                             for (int kb = 0; kb < ksteps; ++kb)
                                 mma_ts(o + ch * 128, w + ch * 128 + kb * 8, v_low + 128u * kb, idesc_o, kb > 0 ? 1u : first);
-                        tc_commit(pv_done);
+                            tc_commit(pv_done(ch));
+                        }
                         tc_commit(kv_free(v.st));
                         tc_commit(o_full);
                         tc_commit(q_free(q.st));
@@ -265,7 +274,7 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             for (int j = 0; j < c.n; ++j, ++sc) {
                 const int p = j & 1;
                 const uint32_t col = s_col + 64 * p;
-                ok = warp_wait(s_full(p), (par >> p) & 1, 0xF10, abort_flag);
+                ok = warp_sleep(s_full(ch, p), (par >> p) & 1, 0xF10, abort_flag);
                 par ^= 1u << p;
                 if (!ok) break;
                 tc_fence_after();
@@ -297,7 +306,7 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                     if (j > 0) {
                         // (the scores of this half block were issued behind the value product before the last: only the last
                         // one's phase can be open)
-                        ok = warp_wait(pv_done, (sc - 1) & 1, 0xF14, abort_flag);
+                        ok = warp_sleep(pv_done(ch), (sc - 1) & 1, 0xF14, abort_flag);
                         if (!ok) break;
                         tc_fence_after();
 #pragma unroll 1
@@ -317,7 +326,7 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 #pragma unroll
                 for (int e = 0; e < 32; ++e) {
                     float2 y = fma2(make_float2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), sl2, nref);
-                    y = e % 4 == 3 ? exp2_poly(y) : exp2_mufu(y);
+                    y = e % 8 == 3 ? exp2_poly(y) : exp2_mufu(y);
                     pk[e] = pack_bf16x2(y.x, y.y);
                     if (e & 1) sum1 = add2(sum1, y); else sum0 = add2(sum0, y);
                 }
@@ -326,7 +335,7 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_full(p));
+                if (lane == 0) mbar_arrive(p_full(ch, p));
             }
             if (!ok) break;
 
@@ -340,8 +349,8 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 s_inv[ch * kRows + r] = inv;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(x_full);
-                ok = warp_wait(x_full, ic & 1, 0xF13, abort_flag);
-                if (ok) ok = warp_wait(o_full, ic & 1, 0xF11, abort_flag);
+                ok = warp_sleep(x_full, ic & 1, 0xF13, abort_flag);
+                if (ok) ok = warp_sleep(o_full, ic & 1, 0xF11, abort_flag);
                 ++ic;
                 i1 = s_inv[r];
                 i2 = s_inv[kRows + r] * lam;

@@ -181,7 +181,24 @@ struct Armed {
     }
 };
 
-// warp-uniform bounded wait of a whole warp
+// Bounded wait whose first tries sleep on the barrier (up to 0.1 ms each; the phase's end wakes them): a wait that spins takes
+// issue slots from the warps that work (8 % of the forward; the backward, whose warps wait less, is 3 % faster with the
+// other).  The slow path stays a call: inlined, the loops outgrow the instruction cache and lose 10 %.
+__device__ __forceinline__ bool sleep_wait(uint32_t bar, uint32_t parity, uint32_t where, volatile uint32_t *abort_flag) {
+    for (int i = 0; i < 4; ++i) {
+        uint32_t ok;
+        asm volatile(
+            "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}"
+            : "=r"(ok) : "r"(bar), "r"(parity), "r"(100000u) : "memory");
+        if (ok) return true;
+    }
+    return mbar_wait_abortable_slow(bar, parity, where, abort_flag);
+}
+// warp-uniform bounded waits of a whole warp
+__device__ __forceinline__ bool warp_sleep(uint32_t bar, uint32_t parity, uint32_t where, volatile uint32_t *abort_flag) {
+    const bool ok = sleep_wait(bar, parity, where, abort_flag);
+    return __all_sync(0xffffffffu, ok);
+}
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, uint32_t where, volatile uint32_t *abort_flag) {
     const bool ok = mbar_wait_abortable(bar, parity, where, abort_flag);
     return __all_sync(0xffffffffu, ok);
