@@ -3,9 +3,10 @@
 //     out = (A_1 - lambda A_2) V,   A_c = softmax(Q_c K_c^T scale o M)
 //
 // Forward (tile kernel): one block per tile of query rows; key tiles go by once, both maps keep a running maximum and
-// sum, the two value sums stay in registers until the end, where they are normalised and subtracted.  16 x 16 threads
-// hold square micro-tiles of both score maps (4 x 4, or 2 x 2 above head dim 128), operands in shared memory; K and V
-// share one buffer so that two blocks fit an SM at head dim 128.
+// sum, the two value sums stay in registers until the end, where they are normalised and subtracted.  The threads
+// hold micro-tiles of both score maps (4 x 4, or 2 x 2 above head dim 128), operands in shared memory; K and V share one
+// buffer.  Up to head dim 64 a block has 32 rows of its own side and 128 threads: more blocks for the small problems that
+// fp32 is used for (2 x 4 heads x 777 rows: 200 blocks instead of 104).
 // Forward (split kernel, few query rows): one block per (KV head, up to 8 query rows, key range); the rows of a GQA
 // group share the K / V tiles it loads.  Its partial sums meet in the combine kernel.
 // Backward: two passes that recompute the maps -- one block per query tile for dQ and the sum for dlambda, one per key
@@ -18,7 +19,6 @@
 namespace ta {
 namespace {
 
-constexpr int kThreads = 256;
 constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ float load1(const float *p) { return __ldg(p); }
@@ -26,51 +26,69 @@ __device__ __forceinline__ float load1(const __nv_bfloat16 *p) { return __bfloat
 __device__ __forceinline__ void store1(float *p, float x) { *p = x; }
 __device__ __forceinline__ void store1(__nv_bfloat16 *p, float x) { *p = __float2bfloat16_rn(x); }
 
+// A block's own side (query rows in the forward and for dQ, keys for dK and dV) and the side it walks.
 template <int DT>
 struct Tile {
-    static constexpr int kRows = DT > 128 ? 32 : 64;   // query rows = keys of a tile
-    static constexpr int kM = kRows / 16;              // micro-tile edge
+    static constexpr int kOwn = DT == 128 ? 64 : 32;
+    static constexpr int kWalk = DT > 128 ? 32 : 64;
+    static constexpr int kThreads = DT == 64 ? 128 : 256;
+    static constexpr int kTy = kThreads / 16;
+    static constexpr int kM = kOwn / kTy;              // a thread's rows: ty + kTy i
+    static constexpr int kN = kWalk / 16;              // and columns of a product of both sides: tx + 16 j
     static constexpr int kLd = DT + 4;                 // floats per operand row (16-byte aligned, conflict-free)
-    static constexpr int kLp = kRows + 4;              // floats per row of a weight tile
-    static constexpr int kCh = DT / 64;                // 4-column chunks per thread of a rows x DT product
+    static constexpr int kLp = kWalk + 4;              // floats per row of a weight tile
+    static constexpr int kCh = DT / 64;                // 4-column chunks per thread of an own side x DT product
 };
 
 // rows [r0, r0 + kRows) of a strided matrix into shared memory as floats; the two halves of the head dim go to columns
-// 0 and DT / 2; rows from `valid` on and the columns between the halves are 0
-template <typename T, int DT>
+// 0 and DT / 2; rows from `valid` on and the columns between the halves are 0.  32 loads of a thread are in flight at
+// once (row after row they took 5600 cycles a tile).
+template <typename T, int DT, int kRows>
 __device__ __forceinline__ void load_tile(float *dst, const T *src, long long stride, int r0, int valid, int D) {
     using C = Tile<DT>;
+    constexpr int kWarps = C::kThreads / 32, kC = DT / 32, kR = kRows / kWarps, kBatch = kR * kC > 32 ? 32 / kC : kR;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = D >> 1;
-    for (int r = warp; r < C::kRows; r += kThreads / 32) {
-        const bool in = r0 + r < valid;
-        const T *row = src + (long long)(r0 + r) * stride;
-        for (int c = lane; c < DT; c += 32) {
-            const int hi = c >= DT / 2 ? 1 : 0, cc = c - hi * (DT / 2);
-            dst[r * C::kLd + c] = (in && cc < half) ? load1(row + hi * half + cc) : 0.f;
+#pragma unroll
+    for (int b = 0; b < kR; b += kBatch) {
+        float v[kBatch][kC];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int r = warp + kWarps * (b + i);
+            const bool in = r0 + r < valid;
+            const T *row = src + (long long)(r0 + r) * stride;
+#pragma unroll
+            for (int j = 0; j < kC; ++j) {
+                const int hi = j >= kC / 2 ? 1 : 0, cc = lane + 32 * (j - hi * (kC / 2));
+                v[i][j] = (in && cc < half) ? load1(row + hi * half + cc) : 0.f;
+            }
         }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+#pragma unroll
+            for (int j = 0; j < kC; ++j) dst[(warp + kWarps * (b + i)) * C::kLd + lane + 32 * j] = v[i][j];
     }
 }
 
-// s[i][j] += A[a_row(i)] . B[b_row(j)] over columns [c0, c1); rows ty + 16 i of A, tx + 16 j of B
+// s[i][j] += A[a_row(i)] . B[b_row(j)] over columns [c0, c1); rows ty + kTy i of A, tx + 16 j of B
 template <int DT>
-__device__ __forceinline__ void dots(const float *A, const float *B, int c0, int c1, float (&s)[Tile<DT>::kM][Tile<DT>::kM]) {
+__device__ __forceinline__ void dots(const float *A, const float *B, int c0, int c1, float (&s)[Tile<DT>::kM][Tile<DT>::kN]) {
     using C = Tile<DT>;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
 #pragma unroll
     for (int i = 0; i < C::kM; ++i)
 #pragma unroll
-        for (int j = 0; j < C::kM; ++j) s[i][j] = 0.f;
+        for (int j = 0; j < C::kN; ++j) s[i][j] = 0.f;
 #pragma unroll 4
     for (int c = c0; c < c1; c += 4) {
-        float4 x[C::kM], y[C::kM];
+        float4 x[C::kM], y[C::kN];
 #pragma unroll
-        for (int i = 0; i < C::kM; ++i) x[i] = *(const float4 *)(A + (ty + 16 * i) * C::kLd + c);
+        for (int i = 0; i < C::kM; ++i) x[i] = *(const float4 *)(A + (ty + C::kTy * i) * C::kLd + c);
 #pragma unroll
-        for (int j = 0; j < C::kM; ++j) y[j] = *(const float4 *)(B + (tx + 16 * j) * C::kLd + c);
+        for (int j = 0; j < C::kN; ++j) y[j] = *(const float4 *)(B + (tx + 16 * j) * C::kLd + c);
 #pragma unroll
         for (int i = 0; i < C::kM; ++i)
 #pragma unroll
-            for (int j = 0; j < C::kM; ++j) {
+            for (int j = 0; j < C::kN; ++j) {
                 s[i][j] = fmaf(x[i].x, y[j].x, s[i][j]);
                 s[i][j] = fmaf(x[i].y, y[j].y, s[i][j]);
                 s[i][j] = fmaf(x[i].z, y[j].z, s[i][j]);
@@ -85,10 +103,10 @@ __device__ __forceinline__ void weighted_rows(const float *W, const float *B, in
     using C = Tile<DT>;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
 #pragma unroll 4
-    for (int u = 0; u < C::kRows; u += 4) {
+    for (int u = 0; u < C::kWalk; u += 4) {
         float4 w[C::kM];
 #pragma unroll
-        for (int i = 0; i < C::kM; ++i) w[i] = *(const float4 *)(W + (ty + 16 * i) * C::kLp + u);
+        for (int i = 0; i < C::kM; ++i) w[i] = *(const float4 *)(W + (ty + C::kTy * i) * C::kLp + u);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float4 b = *(const float4 *)(B + (u + e) * C::kLd + 4 * tx + 64 * ch);
@@ -122,26 +140,26 @@ struct SimtArgs {
 };
 
 template <typename T, int DT>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(Tile<DT>::kThreads)
 diff_simt_kernel(const __grid_constant__ SimtArgs a) {
     using C = Tile<DT>;
     extern __shared__ __align__(16) float sm[];
-    float *sQ = sm, *sKV = sQ + C::kRows * C::kLd, *sP1 = sKV + C::kRows * C::kLd, *sP2 = sP1 + C::kRows * C::kLp;
+    float *sQ = sm, *sKV = sQ + C::kOwn * C::kLd, *sP1 = sKV + C::kWalk * C::kLd, *sP2 = sP1 + C::kOwn * C::kLp;
     const DiffProblem &p = a.p;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
     const int tile = a.tiles - 1 - (int)(blockIdx.x % a.tiles);          // later (longer, when causal) tiles first
     const int bh = (int)(blockIdx.x / a.tiles);
     const int b = bh / p.H, h = bh - b * p.H, hk = h / (p.H / p.H_kv);
     const DiffSpan sp = diff_span(p.q_lens, p.kv_lens, b, p.Nq, p.Nk);
-    const int t0 = tile * C::kRows;
+    const int t0 = tile * C::kOwn;
     const T *qb = (const T *)p.q + b * p.sq.b + h * p.sq.h;
     const T *kb = (const T *)p.k + b * p.sk.b + hk * p.sk.h;
     const T *vb = (const T *)p.v + b * p.sv.b + hk * p.sv.h;
     int row_keys[C::kM], keys_end = 0;
 #pragma unroll
-    for (int i = 0; i < C::kM; ++i) row_keys[i] = sp.keys(t0 + ty + 16 * i, p.causal);
+    for (int i = 0; i < C::kM; ++i) row_keys[i] = sp.keys(t0 + ty + C::kTy * i, p.causal);
     {
-        const int last = min(t0 + C::kRows, sp.ql) - 1;                  // the last valid row sees the most
+        const int last = min(t0 + C::kOwn, sp.ql) - 1;                  // the last valid row sees the most
         keys_end = last >= t0 ? sp.keys(last, p.causal) : 0;
     }
     const float sl = p.scale * kLog2e;
@@ -154,21 +172,21 @@ diff_simt_kernel(const __grid_constant__ SimtArgs a) {
 #pragma unroll
         for (int ch = 0; ch < C::kCh; ++ch) o[0][ch][i] = o[1][ch][i] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    if (keys_end > 0) load_tile<T, DT>(sQ, qb, p.sq.n, t0, sp.ql, p.D);
-    for (int u0 = 0; u0 < keys_end; u0 += C::kRows) {
+    if (keys_end > 0) load_tile<T, DT, C::kOwn>(sQ, qb, p.sq.n, t0, sp.ql, p.D);
+    for (int u0 = 0; u0 < keys_end; u0 += C::kWalk) {
         __syncthreads();
-        load_tile<T, DT>(sKV, kb, p.sk.n, u0, sp.kl, p.D);
+        load_tile<T, DT, C::kWalk>(sKV, kb, p.sk.n, u0, sp.kl, p.D);
         __syncthreads();
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-            float s[C::kM][C::kM];
+            float s[C::kM][C::kN];
             dots<DT>(sQ, sKV, c * (DT / 2), (c + 1) * (DT / 2), s);
             float *sP = c ? sP2 : sP1;
 #pragma unroll
             for (int i = 0; i < C::kM; ++i) {
                 float mx = -INFINITY;
 #pragma unroll
-                for (int j = 0; j < C::kM; ++j) {
+                for (int j = 0; j < C::kN; ++j) {
                     s[i][j] = u0 + tx + 16 * j < row_keys[i] ? s[i][j] * sl : -INFINITY;
                     mx = fmaxf(mx, s[i][j]);
                 }
@@ -178,10 +196,10 @@ diff_simt_kernel(const __grid_constant__ SimtArgs a) {
                 const float alpha = exp2f(m[c][i] - ref);                // 2^-inf = 0 at the first visible key
                 float sum = 0.f;
 #pragma unroll
-                for (int j = 0; j < C::kM; ++j) {
+                for (int j = 0; j < C::kN; ++j) {
                     const float e = exp2f(s[i][j] - ref);
                     sum += e;
-                    sP[(ty + 16 * i) * C::kLp + tx + 16 * j] = e;
+                    sP[(ty + C::kTy * i) * C::kLp + tx + 16 * j] = e;
                 }
 #pragma unroll
                 for (int w = 8; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
@@ -194,7 +212,7 @@ diff_simt_kernel(const __grid_constant__ SimtArgs a) {
             }
         }
         __syncthreads();
-        load_tile<T, DT>(sKV, vb, p.sv.n, u0, sp.kl, p.D);
+        load_tile<T, DT, C::kWalk>(sKV, vb, p.sv.n, u0, sp.kl, p.D);
         __syncthreads();
 #pragma unroll
         for (int ch = 0; ch < C::kCh; ++ch) {
@@ -205,7 +223,7 @@ diff_simt_kernel(const __grid_constant__ SimtArgs a) {
     const float lam = __ldg(p.lambda + (p.lambda_count > 1 ? h : 0));
 #pragma unroll
     for (int i = 0; i < C::kM; ++i) {
-        const int t = t0 + ty + 16 * i;
+        const int t = t0 + ty + C::kTy * i;
         if (t >= p.Nq) continue;
         const bool any = row_keys[i] > 0;
         const float i1 = any ? 1.f / l[0][i] : 0.f, i2 = any ? 1.f / l[1][i] : 0.f;
@@ -590,29 +608,29 @@ diff_stats_kernel(const __grid_constant__ SimtArgs a, float *stats) {
 
 // dQ of one query tile and its share of dlambda: walks the key tiles the rows see
 template <typename T, int DT>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(Tile<DT>::kThreads)
 diff_simt_dq_kernel(const __grid_constant__ SimtArgs a) {
     using C = Tile<DT>;
     extern __shared__ __align__(16) float sm[];
-    float *sQ = sm, *sG = sQ + C::kRows * C::kLd, *sK = sG + C::kRows * C::kLd, *sV = sK + C::kRows * C::kLd;
-    float *sS1 = sV + C::kRows * C::kLd, *sS2 = sS1 + C::kRows * C::kLp;
-    __shared__ float s_red[kThreads / 32];
+    float *sQ = sm, *sG = sQ + C::kOwn * C::kLd, *sK = sG + C::kOwn * C::kLd, *sV = sK + C::kWalk * C::kLd;
+    float *sS1 = sV + C::kWalk * C::kLd, *sS2 = sS1 + C::kOwn * C::kLp;
+    __shared__ float s_red[C::kThreads / 32];
     const DiffProblem &p = a.p;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
     const int tile = a.tiles - 1 - (int)(blockIdx.x % a.tiles);
     const int bh = (int)(blockIdx.x / a.tiles);
     const int b = bh / p.H, h = bh - b * p.H, hk = h / (p.H / p.H_kv);
     const DiffSpan sp = diff_span(p.q_lens, p.kv_lens, b, p.Nq, p.Nk);
-    const int t0 = tile * C::kRows;
+    const int t0 = tile * C::kOwn;
     const T *kb = (const T *)p.k + b * p.sk.b + hk * p.sk.h;
     const T *vb = (const T *)p.v + b * p.sv.b + hk * p.sv.h;
-    const int last = min(t0 + C::kRows, sp.ql) - 1;
+    const int last = min(t0 + C::kOwn, sp.ql) - 1;
     const int keys_end = last >= t0 ? sp.keys(last, p.causal) : 0;
     int row_keys[C::kM];
     float4 st[C::kM];
 #pragma unroll
     for (int i = 0; i < C::kM; ++i) {
-        const int t = t0 + ty + 16 * i;
+        const int t = t0 + ty + C::kTy * i;
         row_keys[i] = sp.keys(t, p.causal);
         st[i] = diff_row_stats(a.g.stats, bh, a.prow, t);          // (padded to whole tiles)
     }
@@ -624,15 +642,15 @@ diff_simt_dq_kernel(const __grid_constant__ SimtArgs a) {
         for (int i = 0; i < C::kM; ++i) dq[ch][i] = make_float4(0.f, 0.f, 0.f, 0.f);
     float dlam = 0.f;
     if (keys_end > 0) {
-        load_tile<T, DT>(sQ, (const T *)p.q + b * p.sq.b + h * p.sq.h, p.sq.n, t0, sp.ql, p.D);
-        load_tile<T, DT>(sG, (const T *)p.dout + b * p.sdo.b + h * p.sdo.h, p.sdo.n, t0, sp.ql, p.D);
+        load_tile<T, DT, C::kOwn>(sQ, (const T *)p.q + b * p.sq.b + h * p.sq.h, p.sq.n, t0, sp.ql, p.D);
+        load_tile<T, DT, C::kOwn>(sG, (const T *)p.dout + b * p.sdo.b + h * p.sdo.h, p.sdo.n, t0, sp.ql, p.D);
     }
-    for (int u0 = 0; u0 < keys_end; u0 += C::kRows) {
+    for (int u0 = 0; u0 < keys_end; u0 += C::kWalk) {
         __syncthreads();
-        load_tile<T, DT>(sK, kb, p.sk.n, u0, sp.kl, p.D);
-        load_tile<T, DT>(sV, vb, p.sv.n, u0, sp.kl, p.D);
+        load_tile<T, DT, C::kWalk>(sK, kb, p.sk.n, u0, sp.kl, p.D);
+        load_tile<T, DT, C::kWalk>(sV, vb, p.sv.n, u0, sp.kl, p.D);
         __syncthreads();
-        float s[C::kM][C::kM], dp[C::kM][C::kM];
+        float s[C::kM][C::kN], dp[C::kM][C::kN];
         dots<DT>(sG, sV, 0, DT, dp);
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
@@ -641,11 +659,11 @@ diff_simt_dq_kernel(const __grid_constant__ SimtArgs a) {
 #pragma unroll
             for (int i = 0; i < C::kM; ++i)
 #pragma unroll
-                for (int j = 0; j < C::kM; ++j) {
+                for (int j = 0; j < C::kN; ++j) {
                     const bool vis = u0 + tx + 16 * j < row_keys[i];
                     const float w = vis ? exp2f(fmaf(s[i][j], sl, c ? st[i].y : st[i].x)) : 0.f;
                     if (c) dlam = fmaf(w, dp[i][j], dlam);
-                    sS[(ty + 16 * i) * C::kLp + tx + 16 * j] = c ? w * (dp[i][j] + st[i].w) * (-lam * p.scale) : w * (dp[i][j] + st[i].z) * p.scale;
+                    sS[(ty + C::kTy * i) * C::kLp + tx + 16 * j] = c ? w * (dp[i][j] + st[i].w) * (-lam * p.scale) : w * (dp[i][j] + st[i].z) * p.scale;
                 }
         }
         __syncthreads();
@@ -654,7 +672,7 @@ diff_simt_dq_kernel(const __grid_constant__ SimtArgs a) {
     }
 #pragma unroll
     for (int i = 0; i < C::kM; ++i) {
-        const int t = t0 + ty + 16 * i;
+        const int t = t0 + ty + C::kTy * i;
         if (t >= p.Nq) continue;
         T *row = (T *)a.g.dq + ((long long)bh * p.Nq + t) * p.D;
 #pragma unroll
@@ -671,20 +689,20 @@ diff_simt_dq_kernel(const __grid_constant__ SimtArgs a) {
     __syncthreads();
     if (threadIdx.x == 0) {
         float x = 0.f;
-        for (int i = 0; i < kThreads / 32; ++i) x += s_red[i];
+        for (int i = 0; i < C::kThreads / 32; ++i) x += s_red[i];
         a.g.dlam_part[(long long)bh * a.tiles + tile] = x;
     }
 }
 
 // dK, dV of one key tile: walks the query heads of its item and, per head, the query tiles that see it
 template <typename T, int DT>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(Tile<DT>::kThreads)
 diff_simt_dkv_kernel(const __grid_constant__ SimtArgs a) {
     using C = Tile<DT>;
     extern __shared__ __align__(16) float sm[];
-    float *sK = sm, *sV = sK + C::kRows * C::kLd, *sQ = sV + C::kRows * C::kLd, *sG = sQ + C::kRows * C::kLd;
-    float *sA = sG + C::kRows * C::kLd, *sS1 = sA + C::kRows * C::kLp, *sS2 = sS1 + C::kRows * C::kLp;
-    __shared__ float4 s_st[C::kRows];
+    float *sK = sm, *sV = sK + C::kOwn * C::kLd, *sQ = sV + C::kOwn * C::kLd, *sG = sQ + C::kWalk * C::kLd;
+    float *sA = sG + C::kWalk * C::kLd, *sS1 = sA + C::kOwn * C::kLp, *sS2 = sS1 + C::kOwn * C::kLp;
+    __shared__ float4 s_st[C::kWalk];
     const DiffProblem &p = a.p;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
     const int tile = (int)(blockIdx.x % a.tiles);                        // earlier (longer, when causal) tiles first
@@ -693,7 +711,7 @@ diff_simt_dkv_kernel(const __grid_constant__ SimtArgs a) {
     const int hk = rest % p.H_kv, b = rest / p.H_kv;
     const int g = p.H / p.H_kv;
     const DiffSpan sp = diff_span(p.q_lens, p.kv_lens, b, p.Nq, p.Nk);
-    const int u0 = tile * C::kRows;
+    const int u0 = tile * C::kOwn;
     const float sl = p.scale * kLog2e;
     float4 dk[C::kCh][C::kM], dv[C::kCh][C::kM];
 #pragma unroll
@@ -701,35 +719,35 @@ diff_simt_dkv_kernel(const __grid_constant__ SimtArgs a) {
 #pragma unroll
         for (int i = 0; i < C::kM; ++i) dk[ch][i] = dv[ch][i] = make_float4(0.f, 0.f, 0.f, 0.f);
     // first row that sees the tile's first key
-    const int t_lo = p.causal ? max(0, u0 - sp.off) / C::kRows * C::kRows : 0;
+    const int t_lo = p.causal ? max(0, u0 - sp.off) / C::kWalk * C::kWalk : 0;
     if (u0 < sp.kl && t_lo < sp.ql) {
-        load_tile<T, DT>(sK, (const T *)p.k + b * p.sk.b + hk * p.sk.h, p.sk.n, u0, sp.kl, p.D);
-        load_tile<T, DT>(sV, (const T *)p.v + b * p.sv.b + hk * p.sv.h, p.sv.n, u0, sp.kl, p.D);
+        load_tile<T, DT, C::kOwn>(sK, (const T *)p.k + b * p.sk.b + hk * p.sk.h, p.sk.n, u0, sp.kl, p.D);
+        load_tile<T, DT, C::kOwn>(sV, (const T *)p.v + b * p.sv.b + hk * p.sv.h, p.sv.n, u0, sp.kl, p.D);
         for (int hh = 0; hh < a.gi; ++hh) {
             const int h = hk * g + hs * a.gi + hh;
             const int bh = b * p.H + h;
             const float lam = __ldg(p.lambda + (p.lambda_count > 1 ? h : 0));
-            for (int t0 = t_lo; t0 < sp.ql; t0 += C::kRows) {
+            for (int t0 = t_lo; t0 < sp.ql; t0 += C::kWalk) {
                 __syncthreads();
-                load_tile<T, DT>(sQ, (const T *)p.q + b * p.sq.b + h * p.sq.h, p.sq.n, t0, sp.ql, p.D);
-                load_tile<T, DT>(sG, (const T *)p.dout + b * p.sdo.b + h * p.sdo.h, p.sdo.n, t0, sp.ql, p.D);
-                if (threadIdx.x < C::kRows) s_st[threadIdx.x] = diff_row_stats(a.g.stats, bh, a.prow, t0 + (int)threadIdx.x);
+                load_tile<T, DT, C::kWalk>(sQ, (const T *)p.q + b * p.sq.b + h * p.sq.h, p.sq.n, t0, sp.ql, p.D);
+                load_tile<T, DT, C::kWalk>(sG, (const T *)p.dout + b * p.sdo.b + h * p.sdo.h, p.sdo.n, t0, sp.ql, p.D);
+                if (threadIdx.x < C::kWalk) s_st[threadIdx.x] = diff_row_stats(a.g.stats, bh, a.prow, t0 + (int)threadIdx.x);
                 __syncthreads();
-                float s[C::kM][C::kM], dp[C::kM][C::kM], w1[C::kM][C::kM];
+                float s[C::kM][C::kN], dp[C::kM][C::kN], w1[C::kM][C::kN];
                 dots<DT>(sV, sG, 0, DT, dp);                             // rows: keys, columns: query rows
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     dots<DT>(sK, sQ, c * (DT / 2), (c + 1) * (DT / 2), s);
                     float *sS = c ? sS2 : sS1;
 #pragma unroll
-                    for (int j = 0; j < C::kM; ++j) {
+                    for (int j = 0; j < C::kN; ++j) {
                         const float4 st = s_st[tx + 16 * j];
                         const int keys = sp.keys(t0 + tx + 16 * j, p.causal);
 #pragma unroll
                         for (int i = 0; i < C::kM; ++i) {
-                            const bool vis = u0 + ty + 16 * i < keys;
+                            const bool vis = u0 + ty + C::kTy * i < keys;
                             const float w = vis ? exp2f(fmaf(s[i][j], sl, c ? st.y : st.x)) : 0.f;
-                            const int at = (ty + 16 * i) * C::kLp + tx + 16 * j;
+                            const int at = (ty + C::kTy * i) * C::kLp + tx + 16 * j;
                             sS[at] = c ? w * (dp[i][j] + st.w) * (-lam * p.scale) : w * (dp[i][j] + st.z) * p.scale;
                             if (c) sA[at] = w1[i][j] - lam * w;
                             else w1[i][j] = w;
@@ -748,7 +766,7 @@ diff_simt_dkv_kernel(const __grid_constant__ SimtArgs a) {
     const long long kv_elems = (long long)p.B * p.H_kv * p.Nk * p.D;
 #pragma unroll
     for (int i = 0; i < C::kM; ++i) {
-        const int u = u0 + ty + 16 * i;
+        const int u = u0 + ty + C::kTy * i;
         if (u >= p.Nk) continue;
         const long long row = (((long long)b * p.H_kv + hk) * p.Nk + u) * p.D;
 #pragma unroll
@@ -822,16 +840,16 @@ int allow_smem(K kern, size_t bytes, PerDeviceOnce &once) {
 template <typename T, int DT>
 int launch_tile(const DiffProblem &p) {
     using C = Tile<DT>;
-    constexpr size_t smem = (2 * C::kRows * C::kLd + 2 * C::kRows * C::kLp) * sizeof(float);
+    constexpr size_t smem = ((C::kOwn + C::kWalk) * C::kLd + 2 * C::kOwn * C::kLp) * sizeof(float);
     static PerDeviceOnce once;
     int rc = allow_smem(diff_simt_kernel<T, DT>, smem, once);
     if (rc != TA_OK) return rc;
     SimtArgs a = {};
     a.p = p;
-    a.tiles = (p.Nq + C::kRows - 1) / C::kRows;
+    a.tiles = (p.Nq + C::kOwn - 1) / C::kOwn;
     const long long blocks = (long long)p.B * p.H * a.tiles;
     if (blocks > 0x7FFFFFFFll) return TA_ERR_TOO_LARGE;
-    return launch_kernel(diff_simt_kernel<T, DT>, (unsigned)blocks, kThreads, smem, p.stream, false, a);
+    return launch_kernel(diff_simt_kernel<T, DT>, (unsigned)blocks, C::kThreads, smem, p.stream, false, a);
 }
 
 template <typename T, int R>
@@ -861,8 +879,8 @@ int launch_split_rows(const DiffProblem &p, const DiffPartials &part) {
 template <typename T, int DT>
 int launch_bwd(const DiffProblem &p, const DiffGrads &g) {
     using C = Tile<DT>;
-    constexpr size_t smem_q = (4 * C::kRows * C::kLd + 2 * C::kRows * C::kLp) * sizeof(float);
-    constexpr size_t smem_k = (4 * C::kRows * C::kLd + 3 * C::kRows * C::kLp) * sizeof(float);
+    constexpr size_t smem_q = (2 * (C::kOwn + C::kWalk) * C::kLd + 2 * C::kOwn * C::kLp) * sizeof(float);
+    constexpr size_t smem_k = (2 * (C::kOwn + C::kWalk) * C::kLd + 3 * C::kOwn * C::kLp) * sizeof(float);
     static PerDeviceOnce once_q, once_k;
     int rc = allow_smem(diff_simt_dq_kernel<T, DT>, smem_q, once_q);
     if (rc == TA_OK) rc = allow_smem(diff_simt_dkv_kernel<T, DT>, smem_k, once_k);
@@ -872,20 +890,20 @@ int launch_bwd(const DiffProblem &p, const DiffGrads &g) {
     a.g = g;
     a.prow = diff_padded_rows(p.Nq);
     a.gi = p.H / p.H_kv / g.hsplit;
-    a.tiles = (p.Nq + C::kRows - 1) / C::kRows;
+    a.tiles = (p.Nq + C::kOwn - 1) / C::kOwn;
     const long long qblocks = (long long)p.B * p.H * a.tiles;
-    const int ktiles = (p.Nk + C::kRows - 1) / C::kRows;
+    const int ktiles = (p.Nk + C::kOwn - 1) / C::kOwn;
     const long long kblocks = (long long)p.B * p.H_kv * g.hsplit * ktiles;
     if (qblocks > 0x7FFFFFFFll || kblocks > 0x7FFFFFFFll) return TA_ERR_TOO_LARGE;
-    rc = launch_kernel(diff_simt_dq_kernel<T, DT>, (unsigned)qblocks, kThreads, smem_q, p.stream, false, a);
+    rc = launch_kernel(diff_simt_dq_kernel<T, DT>, (unsigned)qblocks, C::kThreads, smem_q, p.stream, false, a);
     if (rc != TA_OK) return rc;
     a.tiles = ktiles;
-    return launch_kernel(diff_simt_dkv_kernel<T, DT>, (unsigned)kblocks, kThreads, smem_k, p.stream, false, a);
+    return launch_kernel(diff_simt_dkv_kernel<T, DT>, (unsigned)kblocks, C::kThreads, smem_k, p.stream, false, a);
 }
 
 }  // namespace
 
-int diff_simt_tile(int D) { return D > 128 ? 32 : 64; }
+int diff_simt_tile(int D) { return D <= 64 ? Tile<64>::kOwn : D <= 128 ? Tile<128>::kOwn : Tile<256>::kOwn; }
 
 int launch_diff_simt(const DiffProblem &p) {
     if (p.dtype == TA_DTYPE_F32)
