@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Sequence
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -173,9 +174,9 @@ def load():
     lib.ta_last_cuda_error.argtypes = []
     lib.ta_last_cuda_error.restype = ctypes.c_int
     lib.ta_version.argtypes = []
-    lib.ta_rotary.argtypes = [ctypes.POINTER(ta_rotary_params)]
-    lib.ta_diff_forward.argtypes = [ctypes.POINTER(ta_diff_params)]
-    lib.ta_diff_backward.argtypes = [ctypes.POINTER(ta_diff_bwd_params)]
+    lib.ta_rotary.argtypes = [vp]   # a packed ta_rotary_params
+    lib.ta_diff_forward.argtypes = [vp]   # a packed ta_diff_params
+    lib.ta_diff_backward.argtypes = [vp]   # a packed ta_diff_bwd_params
     lib.ta_diff_workspace_bytes.argtypes = [ci] * 8
     lib.ta_diff_workspace_bytes.restype = ctypes.c_size_t
     for name in EXPORTS:
@@ -204,7 +205,8 @@ def _dims(dims: Sequence[int]):
 def _stream(stream):
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        # (current_stream() builds a Stream object: 2 us of a single-token call)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -364,13 +366,25 @@ def ta_backward_ex(dout, q, k, v, dq, dk, dv, B, H, H_kv, N, D, dims, causal,
     return _done(load().ta_backward_ex(ctypes.byref(p)), "ta_backward_ex", check)
 
 
+def _packer(params):
+    """struct.Struct of a parameter block: packs it in a tenth of the 4 us that the ctypes constructor takes."""
+    codes = {ctypes.c_size_t: "N", ctypes.c_void_p: "P", ctypes.POINTER(ctypes.c_int): "P", ctypes.c_int: "i",
+             ctypes.c_uint: "I", ctypes.c_int64: "q", ctypes.c_double: "d", ctypes.c_float: "f", ctypes.c_int64 * 3: "3q"}
+    s = struct.Struct("@" + "".join(codes[t] for _, t in params._fields_) + "0P")
+    assert s.size == ctypes.sizeof(params)
+    return s
+
+
+_ROTARY_PARAMS, _DIFF_PARAMS, _DIFF_BWD_PARAMS = map(_packer, (ta_rotary_params, ta_diff_params, ta_diff_bwd_params))
+
+
 def _strides(strides, where):
     """(batch, head, token) strides in elements; None: contiguous."""
     if strides is None:
         return (0, 0, 0)
     if len(strides) != 3:
         raise ValueError(f"{where} needs three strides: batch, head, token")
-    return tuple(strides)
+    return strides
 
 
 def ta_rotary(q, k, q_out, k_out, B, H, H_kv, N, D, sections, positions=None, pos_axis_stride=None,
@@ -381,13 +395,15 @@ def ta_rotary(q, k, q_out, k_out, B, H, H_kv, N, D, sections, positions=None, po
     if dims is not None and len(dims) != len(sections):
         raise ValueError("dims and sections need one entry per axis")
     sec, naxes = _dims(sections)
-    p = ta_rotary_params(
-        ctypes.sizeof(ta_rotary_params), _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), B, H, H_kv, N, D, dtype, parts, sec,
-        naxes, _ptr(positions), B * N if pos_axis_stride is None else pos_axis_stride,
-        N if pos_batch_stride is None else pos_batch_stride, None if dims is None else _dims(dims)[0], token_offset, base,
-        int(bool(interleaved)), int(bool(per_axis_ladder)), int(bool(inverse)), _strides(q_strides, "q"),
-        _strides(k_strides, "k"), _strides(q_out_strides, "q_out"), _strides(k_out_strides, "k_out"), _stream(stream))
-    return _done(load().ta_rotary(ctypes.byref(p)), "ta_rotary", check)
+    coords = None if dims is None else _dims(dims)[0]
+    p = _ROTARY_PARAMS.pack(
+        _ROTARY_PARAMS.size, _ptr(q) or 0, _ptr(k) or 0, _ptr(q_out) or 0, _ptr(k_out) or 0, B, H, H_kv, N, D, dtype, parts,
+        ctypes.addressof(sec), naxes, _ptr(positions) or 0, B * N if pos_axis_stride is None else pos_axis_stride,
+        N if pos_batch_stride is None else pos_batch_stride, 0 if coords is None else ctypes.addressof(coords),
+        token_offset, base, bool(interleaved), bool(per_axis_ladder), bool(inverse), *_strides(q_strides, "q"),
+        *_strides(k_strides, "k"), *_strides(q_out_strides, "q_out"), *_strides(k_out_strides, "k_out"),
+        _stream(stream) or 0)
+    return _done(load().ta_rotary(p), "ta_rotary", check)
 
 
 def ta_diff_forward(q, k, v, out, lam, lambda_count, B, H, H_kv, Nq, Nk, D, causal, dtype=TA_DTYPE_BF16,
@@ -395,12 +411,12 @@ def ta_diff_forward(q, k, v, out, lam, lambda_count, B, H, H_kv, Nq, Nk, D, caus
                     out_strides=None, saved=None, workspace=None, workspace_bytes=0, flags=0, stream=None,
                     check=True) -> int:
     """Differential attention; lam: device float32 [lambda_count], lambda_count H or 1."""
-    p = ta_diff_params(
-        ctypes.sizeof(ta_diff_params), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lam), lambda_count, B, H, H_kv, Nq, Nk,
-        D, int(bool(causal)), dtype, softmax_scale, _ptr(q_lens), _ptr(kv_lens), _strides(q_strides, "q"),
-        _strides(k_strides, "k"), _strides(v_strides, "v"), _strides(out_strides, "out"), _ptr(saved), _ptr(workspace),
-        workspace_bytes, flags, _stream(stream))
-    return _done(load().ta_diff_forward(ctypes.byref(p)), "ta_diff_forward", check)
+    p = _DIFF_PARAMS.pack(
+        _DIFF_PARAMS.size, _ptr(q) or 0, _ptr(k) or 0, _ptr(v) or 0, _ptr(out) or 0, _ptr(lam) or 0, lambda_count, B, H,
+        H_kv, Nq, Nk, D, bool(causal), dtype, softmax_scale, _ptr(q_lens) or 0, _ptr(kv_lens) or 0,
+        *_strides(q_strides, "q"), *_strides(k_strides, "k"), *_strides(v_strides, "v"), *_strides(out_strides, "out"),
+        _ptr(saved) or 0, _ptr(workspace) or 0, workspace_bytes, flags, _stream(stream) or 0)
+    return _done(load().ta_diff_forward(p), "ta_diff_forward", check)
 
 
 def ta_diff_backward(dout, q, k, v, out, lam, lambda_count, saved, dq, dk, dv, dlambda, B, H, H_kv, Nq, Nk, D, causal,
@@ -408,13 +424,13 @@ def ta_diff_backward(dout, q, k, v, out, lam, lambda_count, saved, dq, dk, dv, d
                      q_strides=None, k_strides=None, v_strides=None, out_strides=None, workspace=None,
                      workspace_bytes=0, flags=0, stream=None, check=True) -> int:
     """Gradients of ta_diff_forward from what it left in `saved`; dq, dk, dv contiguous, dlambda float32."""
-    p = ta_diff_bwd_params(
-        ctypes.sizeof(ta_diff_bwd_params), _ptr(dout), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lam), lambda_count,
-        _ptr(saved), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dlambda), B, H, H_kv, Nq, Nk, D, int(bool(causal)), dtype,
-        softmax_scale, _ptr(q_lens), _ptr(kv_lens), _strides(dout_strides, "dout"), _strides(q_strides, "q"),
-        _strides(k_strides, "k"), _strides(v_strides, "v"), _strides(out_strides, "out"), _ptr(workspace),
-        workspace_bytes, flags, _stream(stream))
-    return _done(load().ta_diff_backward(ctypes.byref(p)), "ta_diff_backward", check)
+    p = _DIFF_BWD_PARAMS.pack(
+        _DIFF_BWD_PARAMS.size, _ptr(dout) or 0, _ptr(q) or 0, _ptr(k) or 0, _ptr(v) or 0, _ptr(out) or 0, _ptr(lam) or 0,
+        lambda_count, _ptr(saved) or 0, _ptr(dq) or 0, _ptr(dk) or 0, _ptr(dv) or 0, _ptr(dlambda) or 0, B, H, H_kv, Nq,
+        Nk, D, bool(causal), dtype, softmax_scale, _ptr(q_lens) or 0, _ptr(kv_lens) or 0,
+        *_strides(dout_strides, "dout"), *_strides(q_strides, "q"), *_strides(k_strides, "k"), *_strides(v_strides, "v"),
+        *_strides(out_strides, "out"), _ptr(workspace) or 0, workspace_bytes, flags, _stream(stream) or 0)
+    return _done(load().ta_diff_backward(p), "ta_diff_backward", check)
 
 
 def ta_diff_workspace_bytes(B, H, H_kv, Nq, Nk, D, dtype=TA_DTYPE_BF16, mode=TA_DIFF_WS_FORWARD) -> int:

@@ -112,13 +112,13 @@ def _on(device):
     return _SAME_DEVICE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
 
 
-def _strides3(t):
-    return t.stride()[:3]
-
-
-def _row_strided(t):
-    """The tensor itself when the library can address it (innermost features adjacent), else a contiguous copy."""
-    return t if t.stride(3) == 1 or t.shape[3] == 1 else t.contiguous()
+def _strided(t):
+    """(tensor, its three outer strides); a contiguous copy where the innermost features are not adjacent."""
+    b, h, n, d = t.stride()
+    if d == 1 or t.shape[3] == 1:
+        return t, (b, h, n)
+    t = t.contiguous()
+    return t, t.stride()[:3]
 
 
 def _check_rotary(q, k, sections, positions, dims):
@@ -144,13 +144,13 @@ def _check_rotary(q, k, sections, positions, dims):
 def _rotary_call(q, k, sections, positions, dims, token_offset, base, parts, interleaved, per_axis_ladder, inverse):
     import torch
     B, H, N, D = q.shape
-    q = _row_strided(q)
-    q_out = torch.empty((B, H, N, D), dtype=q.dtype, device=q.device)
-    k_out, H_kv = None, 0
+    q, q_strides = _strided(q)
+    q_out = q.new_empty((B, H, N, D))
+    k_out, H_kv, k_strides = None, 0, None
     if k is not None:
-        k = _row_strided(k)
+        k, k_strides = _strided(k)
         H_kv = k.shape[1]
-        k_out = torch.empty((B, H_kv, N, D), dtype=q.dtype, device=q.device)
+        k_out = q.new_empty((B, H_kv, N, D))
     axis = batch = 0
     if positions is not None:
         if positions.stride(-1) != 1 and N > 1:
@@ -158,13 +158,13 @@ def _rotary_call(q, k, sections, positions, dims, token_offset, base, parts, int
         axis = positions.stride(0)
         batch = positions.stride(1) if positions.dim() == 3 else 0
     if q_out.numel() == 0:
-        return q_out, torch.empty_like(k) if k is not None else None
+        return q_out, k_out
     with _on(q.device):
         ta.ta_rotary(q, k, q_out, k_out, B, H, H_kv, N, D, sections, positions=positions, pos_axis_stride=axis,
                      pos_batch_stride=batch, dims=dims, token_offset=token_offset, base=base, parts=parts,
                      interleaved=interleaved, per_axis_ladder=per_axis_ladder, inverse=inverse,
                      dtype=ta.TA_DTYPE_BF16 if q.dtype == torch.bfloat16 else ta.TA_DTYPE_F32,
-                     q_strides=_strides3(q), k_strides=None if k is None else _strides3(k))
+                     q_strides=q_strides, k_strides=k_strides)
     return q_out, k_out
 
 
@@ -236,20 +236,21 @@ def _check_diff(q, k, v, lam, q_lens, kv_lens):
 
 def _diff_forward(q, k, v, lam, causal, softmax_scale, q_lens, kv_lens, save):
     import torch
-    B, H, H_kv, Nq, Nk, D = q.shape[0], q.shape[1], k.shape[1], q.shape[2], k.shape[2], q.shape[3]
+    B, H, Nq, D = q.shape
+    H_kv, Nk = k.shape[1:3]
     dtype = ta.TA_DTYPE_BF16 if q.dtype == torch.bfloat16 else ta.TA_DTYPE_F32
-    out = torch.empty((B, H, Nq, D), dtype=q.dtype, device=q.device)
+    (q, q_strides), (k, k_strides), (v, v_strides) = _strided(q), _strided(k), _strided(v)
+    out = q.new_empty((B, H, Nq, D))
     saved = None
     with _on(q.device):
         if save:
-            saved = torch.empty(ta.ta_diff_workspace_bytes(B, H, H_kv, Nq, Nk, D, dtype, ta.TA_DIFF_WS_SAVED),
-                                dtype=torch.uint8, device=q.device)
+            saved = q.new_empty(ta.ta_diff_workspace_bytes(B, H, H_kv, Nq, Nk, D, dtype, ta.TA_DIFF_WS_SAVED),
+                                dtype=torch.uint8)
         nbytes = ta.ta_diff_workspace_bytes(B, H, H_kv, Nq, Nk, D, dtype, ta.TA_DIFF_WS_FORWARD)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=q.device) if nbytes else None
+        ws = q.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
         ta.ta_diff_forward(q, k, v, out, lam, lam.numel(), B, H, H_kv, Nq, Nk, D, causal, dtype=dtype,
-                           softmax_scale=softmax_scale or 0.0, q_lens=q_lens, kv_lens=kv_lens, q_strides=_strides3(q),
-                           k_strides=_strides3(k), v_strides=_strides3(v), saved=saved, workspace=ws,
-                           workspace_bytes=nbytes)
+                           softmax_scale=softmax_scale or 0.0, q_lens=q_lens, kv_lens=kv_lens, q_strides=q_strides,
+                           k_strides=k_strides, v_strides=v_strides, saved=saved, workspace=ws, workspace_bytes=nbytes)
     return out, saved
 
 
@@ -262,7 +263,7 @@ def _diff_function():
     class _DifferentialAttention(torch.autograd.Function):
         @staticmethod
         def forward(ctx, q, k, v, lam, causal, softmax_scale, q_lens, kv_lens):
-            q, k, v, lam = _row_strided(q), _row_strided(k), _row_strided(v), lam.contiguous()
+            q, k, v, lam = _strided(q)[0], _strided(k)[0], _strided(v)[0], lam.contiguous()
             save = any(ctx.needs_input_grad[:4])
             out, saved = _diff_forward(q, k, v, lam, causal, softmax_scale, q_lens, kv_lens, save)
             if save:
@@ -274,20 +275,19 @@ def _diff_function():
         def backward(ctx, dout):
             q, k, v, lam, out, saved, q_lens, kv_lens = ctx.saved_tensors
             causal, softmax_scale = ctx.args
-            B, H, H_kv, Nq, Nk, D = q.shape[0], q.shape[1], k.shape[1], q.shape[2], k.shape[2], q.shape[3]
+            B, H, Nq, D = q.shape
+            H_kv, Nk = k.shape[1:3]
             dtype = ta.TA_DTYPE_BF16 if q.dtype == torch.bfloat16 else ta.TA_DTYPE_F32
             dout = dout.contiguous()
-            dq = torch.empty((B, H, Nq, D), dtype=q.dtype, device=q.device)
-            dk = torch.empty((B, H_kv, Nk, D), dtype=q.dtype, device=q.device)
-            dv = torch.empty_like(dk)
-            dlam = torch.empty(lam.shape, dtype=torch.float32, device=q.device)
+            dq, dk, dv = q.new_empty((B, H, Nq, D)), q.new_empty((B, H_kv, Nk, D)), q.new_empty((B, H_kv, Nk, D))
+            dlam = lam.new_empty(lam.shape)
             with _on(q.device):
                 nbytes = ta.ta_diff_workspace_bytes(B, H, H_kv, Nq, Nk, D, dtype, ta.TA_DIFF_WS_BACKWARD)
-                ws = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+                ws = q.new_empty(nbytes, dtype=torch.uint8)
                 ta.ta_diff_backward(dout, q, k, v, out, lam, lam.numel(), saved, dq, dk, dv, dlam, B, H, H_kv, Nq, Nk, D,
                                     causal, dtype=dtype, softmax_scale=softmax_scale or 0.0, q_lens=q_lens,
-                                    kv_lens=kv_lens, dout_strides=_strides3(dout), q_strides=_strides3(q),
-                                    k_strides=_strides3(k), v_strides=_strides3(v), workspace=ws,
+                                    kv_lens=kv_lens, dout_strides=dout.stride()[:3], q_strides=q.stride()[:3],
+                                    k_strides=k.stride()[:3], v_strides=v.stride()[:3], workspace=ws,
                                     workspace_bytes=nbytes)
             return dq, dk, dv, dlam, None, None, None, None
 
@@ -306,8 +306,7 @@ def differential_attention(q, k, v, lam, causal=True, softmax_scale=None, q_lens
     global _DIFF
     _check_diff(q, k, v, lam, q_lens, kv_lens)
     if not (q.requires_grad or k.requires_grad or v.requires_grad or lam.requires_grad):
-        return _diff_forward(_row_strided(q), _row_strided(k), _row_strided(v), lam.contiguous(), bool(causal),
-                             softmax_scale, q_lens, kv_lens, False)[0]
+        return _diff_forward(q, k, v, lam.contiguous(), bool(causal), softmax_scale, q_lens, kv_lens, False)[0]
     if _DIFF is None:
         _DIFF = _diff_function()
     return _DIFF.apply(q, k, v, lam, bool(causal), softmax_scale, q_lens, kv_lens)
