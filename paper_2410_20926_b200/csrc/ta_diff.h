@@ -95,6 +95,8 @@ int launch_diff_dlambda(const DiffProblem &p, const DiffGrads &g, int tiles, flo
 // tensor cores: bf16, D = 64 or 128, 16-byte aligned rows (ta_diff_tc.cu)
 int launch_diff_tc(const DiffProblem &p);
 // few query rows: bf16, D = 64 or 128, 16-byte aligned rows (ta_diff_decode.cu)
+// blocks of that kernel that an SM holds (head dim 128: 226 registers a thread)
+inline int diff_decode_resident(int D) { return D > 64 ? 2 : 3; }
 int launch_diff_decode(const DiffProblem &p, const DiffPartials &part);
 int launch_diff_tc_bwd(const DiffProblem &p, const DiffGrads &g);     // (ta_diff_tc_bwd.cu)
 

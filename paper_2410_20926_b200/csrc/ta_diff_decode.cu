@@ -12,6 +12,9 @@
 // so that about 6 KB per warp are always on their way.  A running maximum moves only when it has grown by more than 2^8,
 // which a vote of the warp finds out: the common step has no shuffle.  The weights' second part costs 16 more products and
 // leaves only the result's own rounding.
+// The loads pass by L1 (nothing is read twice): 16 us of 129 for one request with a 128k cache, 32 query heads on 8, D=128,
+// which now takes 95 us, 5.6 TB/s.  None of the arithmetic shows in that time.  Copies through shared memory (cp.async, or TMA
+// into a ring per warp), with twice as much on its way, took 127 to 148 us.
 // The four warps of a block join in shared memory, the blocks of a row in the combine kernel.
 #include "ta_diff_tc.cuh"
 
@@ -40,7 +43,9 @@ __device__ __forceinline__ uint32_t turn8x8(uint32_t x) {
 }
 __device__ __forceinline__ uint4 load16(const __nv_bfloat16 *p, bool in) {
     uint4 v = make_uint4(0, 0, 0, 0);
-    if (in) v = __ldg(reinterpret_cast<const uint4 *>(p));
+    if (in)
+        asm volatile("ld.global.nc.L1::no_allocate.L2::256B.v4.u32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
 __device__ __forceinline__ uint32_t word(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
