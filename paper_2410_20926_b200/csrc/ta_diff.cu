@@ -29,8 +29,8 @@ bool few_rows(int H, int H_kv, int Nq) { return (long long)(H / H_kv) * Nq <= kS
 
 // Key ranges of the split kernels, of 128 keys or more.  Caches of one length (`even`): as many ranges as fill the blocks
 // that are resident together once or twice with the least left over -- a started wave costs a whole one (32 query heads
-// on 8 KV heads, 128k keys: 37 ranges 95 us, 19 ranges a head more 112 us).  Caches of different lengths: six blocks per SM,
-// which even out over the SMs by themselves (32 requests of 1 to 4k keys: 62 us, two per SM 64 us).
+// on 8 KV heads, 128k keys: one full wave 95 us, 1.5 waves 112 us).  Caches of different lengths: six blocks per SM,
+// which even out over the SMs by themselves (32 requests of 1 to 4k keys: 60 us, two per SM 64 us).
 constexpr int kFewestKeys = 128, kMostSplits = 256;
 int num_splits(int B, int H, int H_kv, int Nq, int Nk, int resident, bool even) {
     const long long rows = (long long)(H / H_kv) * Nq, groups = (rows + 7) / 8;
@@ -282,6 +282,7 @@ int backward_impl(const ta_diff_bwd_params &p) {
     g.part = (float *)(ws + L.part);
     g.hsplit = L.hsplit;
     g.dlam_part = (float *)(ws + L.dlam);
+    // (each kernel may start while the one before it drains, and waits for it before it reads)
     if ((rc = launch_diff_stats(d, (float *)(ws + L.stats))) != TA_OK) return rc;
     if ((rc = tc ? launch_diff_tc_bwd(d, g) : launch_diff_simt_bwd(d, g)) != TA_OK) return rc;
     if (g.hsplit > 1 && (rc = launch_diff_group_sum(d, g)) != TA_OK) return rc;

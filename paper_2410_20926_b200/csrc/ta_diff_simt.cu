@@ -608,8 +608,7 @@ diff_stats_kernel(const __grid_constant__ SimtArgs a, float *stats) {
 
 // dQ of one query tile and its share of dlambda: walks the key tiles the rows see
 template <typename T, int DT>
-__global__ void __launch_bounds__(Tile<DT>::kThreads)
-diff_simt_dq_kernel(const __grid_constant__ SimtArgs a) {
+__device__ __forceinline__ void dq_block(const SimtArgs &a, int tiles, int block) {
     using C = Tile<DT>;
     extern __shared__ __align__(16) float sm[];
     float *sQ = sm, *sG = sQ + C::kOwn * C::kLd, *sK = sG + C::kOwn * C::kLd, *sV = sK + C::kWalk * C::kLd;
@@ -617,8 +616,8 @@ diff_simt_dq_kernel(const __grid_constant__ SimtArgs a) {
     __shared__ float s_red[C::kThreads / 32];
     const DiffProblem &p = a.p;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    const int tile = a.tiles - 1 - (int)(blockIdx.x % a.tiles);
-    const int bh = (int)(blockIdx.x / a.tiles);
+    const int tile = tiles - 1 - (int)(block % tiles);
+    const int bh = (int)(block / tiles);
     const int b = bh / p.H, h = bh - b * p.H, hk = h / (p.H / p.H_kv);
     const DiffSpan sp = diff_span(p.q_lens, p.kv_lens, b, p.Nq, p.Nk);
     const int t0 = tile * C::kOwn;
@@ -690,14 +689,13 @@ diff_simt_dq_kernel(const __grid_constant__ SimtArgs a) {
     if (threadIdx.x == 0) {
         float x = 0.f;
         for (int i = 0; i < C::kThreads / 32; ++i) x += s_red[i];
-        a.g.dlam_part[(long long)bh * a.tiles + tile] = x;
+        a.g.dlam_part[(long long)bh * tiles + tile] = x;
     }
 }
 
 // dK, dV of one key tile: walks the query heads of its item and, per head, the query tiles that see it
 template <typename T, int DT>
-__global__ void __launch_bounds__(Tile<DT>::kThreads)
-diff_simt_dkv_kernel(const __grid_constant__ SimtArgs a) {
+__device__ __forceinline__ void dkv_block(const SimtArgs &a, int tiles, int block) {
     using C = Tile<DT>;
     extern __shared__ __align__(16) float sm[];
     float *sK = sm, *sV = sK + C::kOwn * C::kLd, *sQ = sV + C::kOwn * C::kLd, *sG = sQ + C::kWalk * C::kLd;
@@ -705,8 +703,8 @@ diff_simt_dkv_kernel(const __grid_constant__ SimtArgs a) {
     __shared__ float4 s_st[C::kWalk];
     const DiffProblem &p = a.p;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    const int tile = (int)(blockIdx.x % a.tiles);                        // earlier (longer, when causal) tiles first
-    int rest = (int)(blockIdx.x / a.tiles);
+    const int tile = (int)(block % tiles);                        // earlier (longer, when causal) tiles first
+    int rest = (int)(block / tiles);
     const int hs = rest % a.g.hsplit; rest /= a.g.hsplit;
     const int hk = rest % p.H_kv, b = rest / p.H_kv;
     const int g = p.H / p.H_kv;
@@ -786,10 +784,21 @@ diff_simt_dkv_kernel(const __grid_constant__ SimtArgs a) {
     }
 }
 
+// Both passes in one launch: they read the same inputs and write nothing in common, and the small problems that fp32 is
+// used for fill the GPU with neither alone (2 x 4 heads x 777 rows, D=64: 269 us one after the other, 153 us together).
+template <typename T, int DT>
+__global__ void __launch_bounds__(Tile<DT>::kThreads)
+diff_simt_bwd_kernel(const __grid_constant__ SimtArgs a, int ktiles, unsigned kblocks) {
+    griddep_wait();
+    if (blockIdx.x < kblocks) dkv_block<T, DT>(a, ktiles, (int)blockIdx.x);
+    else dq_block<T, DT>(a, a.tiles, (int)(blockIdx.x - kblocks));
+}
+
 // dK, dV = sums of the partials of a group's head chunks, in their order
 template <typename T>
 __global__ void __launch_bounds__(256)
 diff_group_sum_kernel(const float *part, int hsplit, long long n, T *dk, T *dv) {
+    griddep_wait();
     for (long long i = (blockIdx.x * 256ll + threadIdx.x) * 2; i < 2 * n; i += gridDim.x * 512ll) {
         const long long j = i < n ? i : i - n;                 // (n is even: D is)
         const float *src = part + (i < n ? 0 : hsplit * n) + j;
@@ -809,6 +818,7 @@ diff_group_sum_kernel(const float *part, int hsplit, long long n, T *dk, T *dv) 
 // lambda, every thread its terms in order, then a fixed tree
 __global__ void __launch_bounds__(256)
 diff_dlambda_kernel(const float *part, int B, int H, int tiles, int lambda_count, float *dlambda) {
+    griddep_wait();
     __shared__ double s[256];
     double x = 0.;
     const int heads = lambda_count > 1 ? 1 : H;
@@ -879,11 +889,9 @@ int launch_split_rows(const DiffProblem &p, const DiffPartials &part) {
 template <typename T, int DT>
 int launch_bwd(const DiffProblem &p, const DiffGrads &g) {
     using C = Tile<DT>;
-    constexpr size_t smem_q = (2 * (C::kOwn + C::kWalk) * C::kLd + 2 * C::kOwn * C::kLp) * sizeof(float);
-    constexpr size_t smem_k = (2 * (C::kOwn + C::kWalk) * C::kLd + 3 * C::kOwn * C::kLp) * sizeof(float);
-    static PerDeviceOnce once_q, once_k;
-    int rc = allow_smem(diff_simt_dq_kernel<T, DT>, smem_q, once_q);
-    if (rc == TA_OK) rc = allow_smem(diff_simt_dkv_kernel<T, DT>, smem_k, once_k);
+    constexpr size_t smem = (2 * (C::kOwn + C::kWalk) * C::kLd + 3 * C::kOwn * C::kLp) * sizeof(float);
+    static PerDeviceOnce once;
+    const int rc = allow_smem(diff_simt_bwd_kernel<T, DT>, smem, once);
     if (rc != TA_OK) return rc;
     SimtArgs a = {};
     a.p = p;
@@ -894,11 +902,9 @@ int launch_bwd(const DiffProblem &p, const DiffGrads &g) {
     const long long qblocks = (long long)p.B * p.H * a.tiles;
     const int ktiles = (p.Nk + C::kOwn - 1) / C::kOwn;
     const long long kblocks = (long long)p.B * p.H_kv * g.hsplit * ktiles;
-    if (qblocks > 0x7FFFFFFFll || kblocks > 0x7FFFFFFFll) return TA_ERR_TOO_LARGE;
-    rc = launch_kernel(diff_simt_dq_kernel<T, DT>, (unsigned)qblocks, C::kThreads, smem_q, p.stream, false, a);
-    if (rc != TA_OK) return rc;
-    a.tiles = ktiles;
-    return launch_kernel(diff_simt_dkv_kernel<T, DT>, (unsigned)kblocks, C::kThreads, smem_k, p.stream, false, a);
+    if (qblocks + kblocks > 0x7FFFFFFFll) return TA_ERR_TOO_LARGE;
+    return launch_kernel(diff_simt_bwd_kernel<T, DT>, (unsigned)(qblocks + kblocks), C::kThreads, smem, p.stream, true, a, ktiles,
+                         (unsigned)kblocks);
 }
 
 }  // namespace
@@ -955,14 +961,14 @@ int launch_diff_group_sum(const DiffProblem &p, const DiffGrads &g) {
     long long blocks = (n + 255) / 256;
     if (blocks > 148 * 16) blocks = 148 * 16;
     if (p.dtype == TA_DTYPE_F32)
-        return launch_kernel(diff_group_sum_kernel<float>, (unsigned)blocks, 256, 0, p.stream, false, (const float *)g.part,
+        return launch_kernel(diff_group_sum_kernel<float>, (unsigned)blocks, 256, 0, p.stream, true, (const float *)g.part,
                              g.hsplit, n, (float *)g.dk, (float *)g.dv);
-    return launch_kernel(diff_group_sum_kernel<__nv_bfloat16>, (unsigned)blocks, 256, 0, p.stream, false, (const float *)g.part,
+    return launch_kernel(diff_group_sum_kernel<__nv_bfloat16>, (unsigned)blocks, 256, 0, p.stream, true, (const float *)g.part,
                          g.hsplit, n, (__nv_bfloat16 *)g.dk, (__nv_bfloat16 *)g.dv);
 }
 
 int launch_diff_dlambda(const DiffProblem &p, const DiffGrads &g, int tiles, float *dlambda) {
-    return launch_kernel(diff_dlambda_kernel, (unsigned)p.lambda_count, 256, 0, p.stream, false, (const float *)g.dlam_part,
+    return launch_kernel(diff_dlambda_kernel, (unsigned)p.lambda_count, 256, 0, p.stream, true, (const float *)g.dlam_part,
                          p.B, p.H, tiles, p.lambda_count, dlambda);
 }
 

@@ -133,6 +133,7 @@ diff_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    griddep_wait();
     const uint32_t tmem_base = *tmem_slot;
 
     if (warp == 0) {
@@ -444,6 +445,7 @@ diff_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    griddep_wait();
     const uint32_t tmem_base = *tmem_slot;
 
     if (warp < 4) {
@@ -808,13 +810,13 @@ int launch_d(const DiffProblem &p, const DiffGrads &g) {
     a.total_items = (int)dq_items;
     a.tile_major = 2ull * p.B * p.H_kv * p.Nk * D * 2 <= (96ull << 20) ? 1 : 0;
     rc = launch_kernel(diff_tc_dq_kernel<D>, (unsigned)(a.total_items < num_sms ? a.total_items : num_sms), kThreads,
-                       DqCfg<D>::kSmem, p.stream, false, mq, mg, mkh, mvh, a);
+                       DqCfg<D>::kSmem, p.stream, true, mq, mg, mkh, mvh, a);
     if (rc != TA_OK) return rc;
     a.tiles = (p.Nk + kRows - 1) / kRows;
     a.total_items = (int)dkv_items;
     a.tile_major = 2ull * p.B * p.H * p.Nq * D * 2 <= (96ull << 20) ? 1 : 0;
     return launch_kernel(diff_tc_dkv_kernel<D>, (unsigned)(a.total_items < num_sms ? a.total_items : num_sms), kThreads,
-                         DkvCfg<D>::kSmem, p.stream, false, mqh, mgh, mk, mv, a);
+                         DkvCfg<D>::kSmem, p.stream, true, mqh, mgh, mk, mv, a);
 }
 
 }  // namespace
