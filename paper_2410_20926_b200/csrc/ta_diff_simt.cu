@@ -6,7 +6,9 @@
 // sum, the two value sums stay in registers until the end, where they are normalised and subtracted.  The threads
 // hold micro-tiles of both score maps (4 x 4, or 2 x 2 above head dim 128), operands in shared memory; K and V share one
 // buffer.  Up to head dim 64 a block has 32 rows of its own side and 128 threads: more blocks for the small problems that
-// fp32 is used for (2 x 4 heads x 777 rows: 200 blocks instead of 104).
+// fp32 is used for (2 x 4 heads x 777 rows: 200 blocks instead of 104); and as the longest block's walk is what such a
+// problem takes, two groups of those threads walk alternate key tiles and join their sums (107 us alone, 78 us together).
+// Bound by the reads of shared memory (a float4 of either side per 4 products) and, with so few warps, by their latency.
 // Forward (split kernel, few query rows): one block per (KV head, up to 8 query rows, key range); the rows of a GQA
 // group share the K / V tiles it loads.  Its partial sums meet in the combine kernel.
 // Backward: two passes that recompute the maps -- one block per query tile for dQ and the sum for dlambda, one per key
@@ -33,6 +35,7 @@ struct Tile {
     static constexpr int kWalk = DT > 128 ? 32 : 64;
     static constexpr int kThreads = DT == 64 ? 128 : 256;
     static constexpr int kTy = kThreads / 16;
+    static constexpr int kGroups = DT == 64 ? 2 : 1;   // forward: groups of kThreads that walk alternate key tiles
     static constexpr int kM = kOwn / kTy;              // a thread's rows: ty + kTy i
     static constexpr int kN = kWalk / 16;              // and columns of a product of both sides: tx + 16 j
     static constexpr int kLd = DT + 4;                 // floats per operand row (16-byte aligned, conflict-free)
@@ -47,7 +50,7 @@ template <typename T, int DT, int kRows>
 __device__ __forceinline__ void load_tile(float *dst, const T *src, long long stride, int r0, int valid, int D) {
     using C = Tile<DT>;
     constexpr int kWarps = C::kThreads / 32, kC = DT / 32, kR = kRows / kWarps, kBatch = kR * kC > 32 ? 32 / kC : kR;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = D >> 1;
+    const int warp = (threadIdx.x % C::kThreads) >> 5, lane = threadIdx.x & 31, half = D >> 1;
 #pragma unroll
     for (int b = 0; b < kR; b += kBatch) {
         float v[kBatch][kC];
@@ -73,7 +76,7 @@ __device__ __forceinline__ void load_tile(float *dst, const T *src, long long st
 template <int DT>
 __device__ __forceinline__ void dots(const float *A, const float *B, int c0, int c1, float (&s)[Tile<DT>::kM][Tile<DT>::kN]) {
     using C = Tile<DT>;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    const int tx = threadIdx.x & 15, ty = (threadIdx.x % C::kThreads) >> 4;
 #pragma unroll
     for (int i = 0; i < C::kM; ++i)
 #pragma unroll
@@ -101,7 +104,7 @@ __device__ __forceinline__ void dots(const float *A, const float *B, int c0, int
 template <int DT>
 __device__ __forceinline__ void weighted_rows(const float *W, const float *B, int ch, float4 (&acc)[Tile<DT>::kM]) {
     using C = Tile<DT>;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    const int tx = threadIdx.x & 15, ty = (threadIdx.x % C::kThreads) >> 4;
 #pragma unroll 4
     for (int u = 0; u < C::kWalk; u += 4) {
         float4 w[C::kM];
@@ -118,6 +121,37 @@ __device__ __forceinline__ void weighted_rows(const float *W, const float *B, in
                 acc[i].z = fmaf(x, b.z, acc[i].z);
                 acc[i].w = fmaf(x, b.w, acc[i].w);
             }
+        }
+    }
+}
+
+// the same with two sets of weights, which share the reads of B
+template <int DT>
+__device__ __forceinline__ void weighted_rows(const float *W1, const float *W2, const float *B, int ch, float4 (&acc)[2][Tile<DT>::kCh][Tile<DT>::kM]) {
+    using C = Tile<DT>;
+    const int tx = threadIdx.x & 15, ty = (threadIdx.x % C::kThreads) >> 4;
+#pragma unroll 2
+    for (int u = 0; u < C::kWalk; u += 4) {
+        float4 w[2][C::kM];
+#pragma unroll
+        for (int i = 0; i < C::kM; ++i) {
+            w[0][i] = *(const float4 *)(W1 + (ty + C::kTy * i) * C::kLp + u);
+            w[1][i] = *(const float4 *)(W2 + (ty + C::kTy * i) * C::kLp + u);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float4 b = *(const float4 *)(B + (u + e) * C::kLd + 4 * tx + 64 * ch);
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int i = 0; i < C::kM; ++i) {
+                    const float x = e == 0 ? w[c][i].x : e == 1 ? w[c][i].y : e == 2 ? w[c][i].z : w[c][i].w;
+                    float4 &y = acc[c][ch][i];
+                    y.x = fmaf(x, b.x, y.x);
+                    y.y = fmaf(x, b.y, y.y);
+                    y.z = fmaf(x, b.z, y.z);
+                    y.w = fmaf(x, b.w, y.w);
+                }
         }
     }
 }
@@ -139,14 +173,24 @@ struct SimtArgs {
     long long prow;            // padded rows of the statistics
 };
 
+template <int DT>
+constexpr int kTileFloats = (Tile<DT>::kOwn + Tile<DT>::kWalk) * Tile<DT>::kLd + 2 * Tile<DT>::kOwn * Tile<DT>::kLp;
+template <int DT>
+__device__ __forceinline__ void group_sync(int group) {
+    if constexpr (Tile<DT>::kGroups > 1) asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(Tile<DT>::kThreads) : "memory");
+    else __syncthreads();
+}
+
 template <typename T, int DT>
-__global__ void __launch_bounds__(Tile<DT>::kThreads)
+__global__ void __launch_bounds__(Tile<DT>::kThreads *Tile<DT>::kGroups)
 diff_simt_kernel(const __grid_constant__ SimtArgs a) {
     using C = Tile<DT>;
-    extern __shared__ __align__(16) float sm[];
+    extern __shared__ __align__(16) float smem[];
+    const int group = threadIdx.x / C::kThreads, tid = threadIdx.x % C::kThreads;
+    float *sm = smem + group * kTileFloats<DT>;
     float *sQ = sm, *sKV = sQ + C::kOwn * C::kLd, *sP1 = sKV + C::kWalk * C::kLd, *sP2 = sP1 + C::kOwn * C::kLp;
     const DiffProblem &p = a.p;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    const int tx = tid & 15, ty = tid >> 4;
     const int tile = a.tiles - 1 - (int)(blockIdx.x % a.tiles);          // later (longer, when causal) tiles first
     const int bh = (int)(blockIdx.x / a.tiles);
     const int b = bh / p.H, h = bh - b * p.H, hk = h / (p.H / p.H_kv);
@@ -173,10 +217,10 @@ diff_simt_kernel(const __grid_constant__ SimtArgs a) {
         for (int ch = 0; ch < C::kCh; ++ch) o[0][ch][i] = o[1][ch][i] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
     if (keys_end > 0) load_tile<T, DT, C::kOwn>(sQ, qb, p.sq.n, t0, sp.ql, p.D);
-    for (int u0 = 0; u0 < keys_end; u0 += C::kWalk) {
-        __syncthreads();
+    for (int u0 = group * C::kWalk; u0 < keys_end; u0 += C::kGroups * C::kWalk) {
+        group_sync<DT>(group);
         load_tile<T, DT, C::kWalk>(sKV, kb, p.sk.n, u0, sp.kl, p.D);
-        __syncthreads();
+        group_sync<DT>(group);
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             float s[C::kM][C::kN];
@@ -211,14 +255,42 @@ diff_simt_kernel(const __grid_constant__ SimtArgs a) {
                 }
             }
         }
-        __syncthreads();
+        group_sync<DT>(group);
         load_tile<T, DT, C::kWalk>(sKV, vb, p.sv.n, u0, sp.kl, p.D);
-        __syncthreads();
+        group_sync<DT>(group);
 #pragma unroll
-        for (int ch = 0; ch < C::kCh; ++ch) {
-            weighted_rows<DT>(sP1, sKV, ch, o[0][ch]);
-            weighted_rows<DT>(sP2, sKV, ch, o[1][ch]);
+        for (int ch = 0; ch < C::kCh; ++ch) weighted_rows<DT>(sP1, sP2, sKV, ch, o);
+    }
+    if constexpr (C::kGroups > 1) {
+        // the second group's sums join the first's
+        float *sO = smem + kTileFloats<DT>, *sML = sO + 2 * C::kOwn * DT;
+        if (group) {
+            group_sync<DT>(group);
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int i = 0; i < C::kM; ++i) {
+                    const int r = c * C::kOwn + ty + C::kTy * i;
+                    *(float4 *)(sO + r * DT + 4 * tx) = o[c][0][i];
+                    if (tx == 0) *(float2 *)(sML + 2 * r) = make_float2(m[c][i], l[c][i]);
+                }
         }
+        __syncthreads();
+        if (group) return;
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int i = 0; i < C::kM; ++i) {
+                const int r = c * C::kOwn + ty + C::kTy * i;
+                const float2 ml = *(const float2 *)(sML + 2 * r);
+                const float4 x = *(const float4 *)(sO + r * DT + 4 * tx);
+                const float mn = fmaxf(m[c][i], ml.x), ref = mn == -INFINITY ? 0.f : mn;
+                const float f0 = exp2f(m[c][i] - ref), f1 = exp2f(ml.x - ref);
+                m[c][i] = mn;
+                l[c][i] = l[c][i] * f0 + ml.y * f1;
+                float4 &y = o[c][0][i];
+                y = make_float4(y.x * f0 + x.x * f1, y.y * f0 + x.y * f1, y.z * f0 + x.z * f1, y.w * f0 + x.w * f1);
+            }
     }
     const float lam = __ldg(p.lambda + (p.lambda_count > 1 ? h : 0));
 #pragma unroll
@@ -850,7 +922,8 @@ int allow_smem(K kern, size_t bytes, PerDeviceOnce &once) {
 template <typename T, int DT>
 int launch_tile(const DiffProblem &p) {
     using C = Tile<DT>;
-    constexpr size_t smem = ((C::kOwn + C::kWalk) * C::kLd + 2 * C::kOwn * C::kLp) * sizeof(float);
+    constexpr size_t smem = C::kGroups * kTileFloats<DT> * sizeof(float);
+    static_assert(C::kGroups == 1 || kTileFloats<DT> >= 2 * C::kOwn * (DT + 2), "the sums fit where the tiles were");
     static PerDeviceOnce once;
     int rc = allow_smem(diff_simt_kernel<T, DT>, smem, once);
     if (rc != TA_OK) return rc;
@@ -859,7 +932,7 @@ int launch_tile(const DiffProblem &p) {
     a.tiles = (p.Nq + C::kOwn - 1) / C::kOwn;
     const long long blocks = (long long)p.B * p.H * a.tiles;
     if (blocks > 0x7FFFFFFFll) return TA_ERR_TOO_LARGE;
-    return launch_kernel(diff_simt_kernel<T, DT>, (unsigned)blocks, C::kThreads, smem, p.stream, false, a);
+    return launch_kernel(diff_simt_kernel<T, DT>, (unsigned)blocks, C::kThreads * C::kGroups, smem, p.stream, false, a);
 }
 
 template <typename T, int R>
