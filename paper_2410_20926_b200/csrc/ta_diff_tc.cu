@@ -16,14 +16,22 @@
 // h, then S of half block h + 2 into the slot this frees, chain after chain --, warps 4-7 and 8-11 are the softmax of
 // chain 1 and 2 (one query row per thread).  The chains run half a step apart, so that one is at its maxima while the
 // other keeps the special-function units busy (in step they were 15 % slower).  The issuing thread's own instructions,
-// above all its waits (about 100 cycles each) and commits, have to fit beside the products.  An eighth of the exponentials are polynomials on the multiply-add pipes (exp2_poly).  A
-// running maximum is moved (and O rescaled) only when it has grown by more than 2^8: weights up to 256 lose nothing in
-// bf16 or fp32.  Every wait is bounded; when one expires the CTA raises a flag that ends all roles, lets its copies land,
-// frees its tensor memory and returns.
+// above all its waits (about 100 cycles each) and commits, have to fit beside the products.  An eighth of the exponentials
+// are polynomials on the multiply-add pipes (exp2_poly).  A running maximum is moved (and O rescaled) only when it has
+// grown by more than 2^8: weights up to 256 lose nothing in bf16 or fp32.  Every wait is bounded; when one expires the CTA
+// raises a flag that ends all roles, lets its copies land, frees its tensor memory and returns.
+//
+// Rounding: the weights become bf16 to be operands of the value product (both operands have one type, and V is bf16); their
+// sums l, the scores and O stay fp32.  Each weight is off by at most 2^-9 of itself, independently, which leaves the result
+// about as far off as its own rounding to bf16 does (both together 1.5 times that alone).  A second product with what the
+// rounding left would remove it at 8 D more multiply-adds a pair instead of 6 D; the kernels for few rows, which wait for
+// memory, do that.
 //
 // Per 128 x 128 pairs of rows and keys and both maps, in cycles: MMAs 1792 (a 128 x 64 product from shared memory takes 48
 // where the pipe would need 32: reading its operands bounds it), exponentials 2048 on the special-function unit alone,
-// 1536 so.
+// 1792 so; measured about 2900 -- each scheduler has two softmax warps, whose loads of scores, maxima and stores of weights
+// wait for one another.  16k causal tokens, H = 8, D = 128: 735 us, 748 TFLOP/s of the definition's products (half the
+// burst rate of a library product, whose ceiling here is 2/3 as the pass does 6 D for 4 D).
 #include "ta_diff_tc.cuh"
 
 namespace ta {
