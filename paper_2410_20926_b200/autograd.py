@@ -182,6 +182,7 @@ def _rotary_function():
             return _rotary_call(q, k, args[0], positions, *args[1:], False)
 
         @staticmethod
+        @torch.autograd.function.once_differentiable
         def backward(ctx, dq, dk):
             (positions,) = ctx.saved_tensors
             dq, dk = _rotary_call(dq, dk, ctx.args[0], positions, *ctx.args[1:], True)
@@ -272,6 +273,7 @@ def _diff_function():
             return out
 
         @staticmethod
+        @torch.autograd.function.once_differentiable
         def backward(ctx, dout):
             q, k, v, lam, out, saved, q_lens, kv_lens = ctx.saved_tensors
             causal, softmax_scale = ctx.args

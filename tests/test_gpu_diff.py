@@ -337,3 +337,54 @@ def test_training_run_with_rotary():
         near(name, g, (rotate(val, ang, 2, False, inverse=True), 2 * both + 16 * ref.U32 * np.abs(val).max()))
     near("dv", grads[2], (want["dv"][0], 2 * want["dv"][1]))
     near("dlam", grads[3], (want["dlam"][0], 2 * want["dlam"][1]))
+
+
+@pytest.mark.parametrize("shape", [
+    (1, 8, 8, 1, 5000, 128), (1, 4, 4, 1, 5000, 64), (3, 8, 2, 1, 2049, 128), (40, 8, 8, 1, 300, 128), (60, 8, 8, 1, 260, 64),
+    (1, 8, 1, 4, 9000, 128), (1, 1, 1, 1, 40000, 128),
+])
+def test_key_ranges_of_few_rows(shape):
+    """Caches of one length (ranges that fill waves of blocks) and of several, fewer and more blocks than one wave."""
+    B, Nk = shape[0], shape[4]
+    check(*shape, grad=False)
+    check(*shape, grad=False, kl=[Nk - 37 * i % Nk for i in range(B)])
+
+
+@pytest.mark.parametrize("dtype,D", [("bfloat16", 128), ("float32", 64)])
+def test_offsets_beyond_32_bits(dtype, D):
+    """Tokens 2^20 elements apart: the last of 2100 stand behind element 2^31."""
+    import torch
+    N, step = 2100, 1 << 20
+    big = torch.empty(N * step, dtype=getattr(torch, dtype), device="cuda")
+    k, v = big.as_strided((1, 2, N, D), (0, D, step, 1)), big.as_strided((1, 2, N, D), (0, D, step, 1), 2 * D)
+    q = big.as_strided((1, 4, N, D), (0, D, step, 1), 4 * D)
+    for i, t in enumerate((k, v, q)):
+        t.copy_(draw(70 + i, tuple(t.shape), dtype=dtype)[0])
+    lam = lambdas(73, 4)
+    leaves = [t.clone(memory_format=torch.contiguous_format).requires_grad_() for t in (q, k, v)]
+    far = [t.detach().requires_grad_() for t in (q, k, v)]
+    for rows in (slice(N - 130, N), slice(N - 2, N)):
+        outs = [ta.differential_attention(a[:, :, rows], b, c, lam) for a, b, c in (leaves, far)]
+        assert torch.equal(outs[0], outs[1])
+        do, = draw(74, tuple(outs[0].shape), dtype=dtype)
+        for a, b in zip(torch.autograd.grad(outs[0], leaves, do), torch.autograd.grad(outs[1], far, do)):
+            assert torch.equal(a, b)
+    # the result's own rows as far apart
+    far_out = big.as_strided((1, 4, N, D), (0, D, step, 1), 8 * D)
+    for rows in (N, 2):
+        args = (q[:, :, N - rows:], leaves[1], leaves[2])
+        far_rows = far_out[:, :, N - rows:]
+        ta.ta_diff_forward(args[0], args[1], args[2], far_rows, lam, 4, 1, 4, 2, rows, N, D, True,
+                           dtype=ta.TA_DTYPE_BF16 if dtype == "bfloat16" else ta.TA_DTYPE_F32,
+                           q_strides=args[0].stride()[:3], out_strides=far_rows.stride()[:3])
+        with torch.no_grad():
+            assert torch.equal(far_rows, ta.differential_attention(*args, lam))
+
+
+def test_second_derivatives_are_refused():
+    import torch
+    q, k, v = (t.requires_grad_() for t in draw(80, (1, 2, 8, 64), (1, 2, 8, 64), (1, 2, 8, 64)))
+    out = ta.differential_attention(q, k, v, lambdas(81, 2))
+    dq, = torch.autograd.grad(out.float().square().sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError):
+        dq.float().sum().backward()

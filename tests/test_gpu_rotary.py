@@ -178,3 +178,30 @@ def test_captured_on_another_stream_and_empty():
     assert torch.equal(gq, qo) and torch.equal(gk, ko)
     e, f = ta.multi_axis_rotary(q[:0], k[:0], (16, 24, 24), positions=pos[:, :0])
     assert e.shape == (0, 8, 1, 128) and f.shape == (0, 2, 1, 128)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_offsets_beyond_32_bits(dtype):
+    """Tokens 2^20 elements apart, in place: the last of 2100 stand behind element 2^31."""
+    import torch
+    N, step, D = 2100, 1 << 20, 64
+    big = torch.empty(N * step, dtype=getattr(torch, dtype), device="cuda")
+    q, k = big.as_strided((1, 3, N, D), (0, D, step, 1)), big.as_strided((1, 1, N, D), (0, D, step, 1), 3 * D)
+    q.copy_(dev((1, 3, N, D), 20, dtype))
+    k.copy_(dev((1, 1, N, D), 21, dtype))
+    near = [t.clone(memory_format=torch.contiguous_format) for t in (q, k)]
+    want = ta.multi_axis_rotary(*near, (16, 16), dims=(42, 50))
+    for got, w in zip(ta.multi_axis_rotary(q, k, (16, 16), dims=(42, 50)), want):
+        assert torch.equal(got, w)
+    ta.ta_rotary(q, k, q, k, 1, 3, 1, N, D, (16, 16), dims=(42, 50), q_strides=q.stride()[:3], k_strides=k.stride()[:3],
+                 q_out_strides=q.stride()[:3], k_out_strides=k.stride()[:3],
+                 dtype=ta.TA_DTYPE_BF16 if dtype == "bfloat16" else ta.TA_DTYPE_F32)
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1])
+
+
+def test_second_derivatives_are_refused():
+    import torch
+    q = dev((1, 1, 4, 8), 22, "float32").requires_grad_()
+    g, = torch.autograd.grad(ta.multi_axis_rotary(q, None, (4,), dims=(4,))[0].square().sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.sum().backward()
