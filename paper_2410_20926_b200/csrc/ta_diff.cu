@@ -27,42 +27,22 @@ int check_shape(int B, int H, int H_kv, int Nq, int Nk, int D, int dtype) {
 
 bool few_rows(int H, int H_kv, int Nq) { return (long long)(H / H_kv) * Nq <= kSplitRows; }
 
-// Key ranges of the split kernels, of 128 keys or more.  Caches of one length (`even`): as many ranges as fill the blocks
-// that are resident together once or twice with the least left over -- a started wave costs a whole one (32 query heads
-// on 8 KV heads, 128k keys: one full wave 95 us, 1.5 waves 112 us).  Caches of different lengths: six blocks per SM,
-// which even out over the SMs by themselves (32 requests of 1 to 4k keys: 60 us, two per SM 64 us).
-constexpr int kFewestKeys = 128, kMostSplits = 256;
-int num_splits(int B, int H, int H_kv, int Nq, int Nk, int resident, bool even) {
-    const long long rows = (long long)(H / H_kv) * Nq, groups = (rows + 7) / 8;
-    const long long blocks = (long long)B * H_kv * groups, sms = current_device_sms(nullptr);
-    long long most = ((long long)Nk + kFewestKeys - 1) / kFewestKeys;
-    if (most > kMostSplits) most = kMostSplits;
-    if (!even) {
-        const long long s = (6 * sms + blocks - 1) / blocks;
-        return (int)(s < most ? s : most);
-    }
-    const long long slots = resident * sms;
-    if (most > 2 * slots / blocks) most = 2 * slots / blocks;
-    int best = 1;
-    double filled = 0.;
-    for (int s = 1; s <= most; ++s) {
-        const long long n = blocks * s, waves = (n + slots - 1) / slots;
-        const double f = (double)n / (double)(waves * slots);
-        if (f > filled + 0.01) {
-            filled = f;
-            best = s;
-        }
-    }
-    return best;
+long long row_groups(int H, int H_kv, int Nq) { return ((long long)(H / H_kv) * Nq + kDiffGroupRows - 1) / kDiffGroupRows; }
+// Key ranges of the CUDA-core split kernel: six blocks per SM, ranges of 256 keys or more.
+int num_splits(int B, int H, int H_kv, int Nq, int Nk) {
+    const long long blocks = (long long)B * H_kv * row_groups(H, H_kv, Nq);
+    const long long want = 6ll * current_device_sms(nullptr);
+    long long s = (want + blocks - 1) / blocks;
+    const long long most = ((long long)Nk + 255) / 256;
+    if (s > most) s = most;
+    if (s > 256) s = 256;
+    return s < 1 ? 1 : (int)s;
 }
-// the most ranges that any of these rules gives: what the workspace holds
-int most_splits(int B, int H, int H_kv, int Nq, int Nk) {
-    int s = num_splits(B, H, H_kv, Nq, Nk, 0, false);
-    for (int resident : {diff_decode_resident(64), diff_decode_resident(128)}) {
-        const int x = num_splits(B, H, H_kv, Nq, Nk, resident, true);
-        if (x > s) s = x;
-    }
-    return s;
+// Shares of the tensor-core kernel: one per block that is resident, of 128 keys or more.
+int num_shares(int B, int H, int H_kv, int Nq, int Nk, int D) {
+    const long long most = (long long)B * H_kv * row_groups(H, H_kv, Nq) * (((long long)Nk + 127) / 128);
+    const long long n = (long long)diff_decode_resident(D) * current_device_sms(nullptr);
+    return (int)(n < most ? n : most);
 }
 
 // Head chunks of a GQA group whose dK, dV partials are kept apart: the group is split while its items are fewer than
@@ -99,11 +79,25 @@ void set_saved(DiffProblem *d, void *saved) {
     }
 }
 
-size_t forward_bytes(int B, int H, int H_kv, int Nq, int Nk, int D) {
-    if (!few_rows(H, H_kv, Nq)) return 0;
-    const size_t slots = (size_t)B * H * Nq * most_splits(B, H, H_kv, Nq, Nk);
-    return up256(slots * sizeof(float4)) + up256(slots * 2 * D * sizeof(float));
+// (which kernel runs also depends on the addresses: the workspace is large enough for either)
+struct ForwardLayout {
+    size_t acc, first, total;
+    int rows_per_slot;
+};
+ForwardLayout forward_layout(int B, int H, int H_kv, int Nq, int Nk, int D) {
+    ForwardLayout L = {};
+    if (!few_rows(H, H_kv, Nq)) return L;
+    const size_t rows = (size_t)(H / H_kv) * Nq, pairs = (size_t)B * H_kv * row_groups(H, H_kv, Nq);
+    L.rows_per_slot = (int)(rows < (size_t)kDiffGroupRows ? rows : (size_t)kDiffGroupRows);
+    size_t slots = (size_t)B * H * Nq * num_splits(B, H, H_kv, Nq, Nk);
+    const size_t shared = (pairs + num_shares(B, H, H_kv, Nq, Nk, D)) * L.rows_per_slot;
+    if (shared > slots) slots = shared;
+    L.acc = up256(slots * sizeof(float4));
+    L.first = L.acc + up256(slots * 2 * D * sizeof(float));
+    L.total = L.first + up256(pairs * sizeof(int2));
+    return L;
 }
+size_t forward_bytes(int B, int H, int H_kv, int Nq, int Nk, int D) { return forward_layout(B, H, H_kv, Nq, Nk, D).total; }
 
 struct BackwardLayout {
     size_t stats, dlam, part, total;
@@ -228,10 +222,18 @@ int forward_impl(const ta_diff_params &p) {
         if ((rc = pool_alloc(need, d.stream, &pooled.ptr)) != TA_OK) return rc;
         ws = (char *)pooled.ptr;
     }
-    DiffPartials part;
-    part.splits = num_splits(p.B, p.H, p.H_kv, p.Nq, p.Nk, diff_decode_resident(p.D), tc && !p.kv_lens);
+    const ForwardLayout L = forward_layout(p.B, p.H, p.H_kv, p.Nq, p.Nk, p.D);
+    DiffPartials part = {};
     part.ml = (float4 *)ws;
-    part.acc = (float *)(ws + up256((size_t)p.B * p.H * p.Nq * part.splits * sizeof(float4)));
+    part.acc = (float *)(ws + L.acc);
+    if (tc) {
+        part.first = (int2 *)(ws + L.first);
+        part.shares = num_shares(p.B, p.H, p.H_kv, p.Nq, p.Nk, p.D);
+        part.groups = (int)row_groups(p.H, p.H_kv, p.Nq);
+        part.rows_per_slot = L.rows_per_slot;
+    } else {
+        part.splits = num_splits(p.B, p.H, p.H_kv, p.Nq, p.Nk);
+    }
     if ((rc = tc ? launch_diff_decode(d, part) : launch_diff_simt_split(d, part)) != TA_OK) return rc;
     return launch_diff_combine(d, part);
 }

@@ -56,12 +56,16 @@ __device__ __forceinline__ uint32_t diff_pack16(float a, float b) {
     return ((uint32_t)__float2int_rn(a) & 0xFFFFu) | ((uint32_t)__float2int_rn(b) << 16);
 }
 
-// Buffers of one call behind the forward's workspace: partial results of `splits` key ranges per query row,
-// [row][split]: (m_1, l_1, m_2, l_2) and the two un-normalised value sums, D floats each.
+// Buffers of one call behind the forward's workspace: partial results of key ranges.  Either `splits` ranges for every
+// query row, or (`shares` given) equal shares of all the work, one per block of the grid.  Then a pair (batch entry, group of
+// up to 8 rows of a KV head) has the slots first[pair].x and on, first[pair].y of them, of rows_per_slot rows each.
+constexpr int kDiffGroupRows = 8;
 struct DiffPartials {
     float4 *ml;
     float *acc;
     int splits;
+    int2 *first;
+    int shares, groups, rows_per_slot;
 };
 
 // Row statistics of the backward: -lse_1, -lse_2, -d_1, -d_2 (as the kernels add them), 64 rows of each in turn, so that
@@ -95,7 +99,7 @@ int launch_diff_dlambda(const DiffProblem &p, const DiffGrads &g, int tiles, flo
 // tensor cores: bf16, D = 64 or 128, 16-byte aligned rows (ta_diff_tc.cu)
 int launch_diff_tc(const DiffProblem &p);
 // few query rows: bf16, D = 64 or 128, 16-byte aligned rows (ta_diff_decode.cu)
-// blocks of that kernel that an SM holds (head dim 128: 226 registers a thread)
+// blocks of that kernel that an SM holds (head dim 128: more than 168 registers a thread)
 inline int diff_decode_resident(int D) { return D > 64 ? 2 : 3; }
 int launch_diff_decode(const DiffProblem &p, const DiffPartials &part);
 int launch_diff_tc_bwd(const DiffProblem &p, const DiffGrads &g);     // (ta_diff_tc_bwd.cu)

@@ -13,20 +13,25 @@
 // which a vote of the warp finds out: the common step has no shuffle.  The weights' second part costs 16 more products and
 // leaves only the result's own rounding.
 // The loads pass by L1 (nothing is read twice): 16 us of 129 for one request with a 128k cache, 32 query heads on 8, D=128,
-// which now takes 95 us, 5.6 TB/s.  None of the arithmetic shows in that time.  Copies through shared memory (cp.async, or TMA
+// which now takes 97 us, 5.5 TB/s.  None of the arithmetic shows in that time.  Copies through shared memory (cp.async, or TMA
 // into a ring per warp), with twice as much on its way, took 127 to 148 us.
-// The four warps of a block join in shared memory, the blocks of a row in the combine kernel.
+// The four warps of a block join in shared memory, the ranges of a row in the combine kernel.
+// The blocks that are resident take equal shares of the keys of all entries and KV heads, which they work out from the
+// lengths: one wave, no block longer than another.  (Equal numbers of ranges for every request, six blocks per SM: 60 us for
+// 32 requests of 1 to 4k keys instead of 56, 198 instead of 186 for 64 of 1 to 8k, 44 instead of 38 for 8 of 1 to 32k at D=64.)
 #include "ta_diff_tc.cuh"
 
 namespace ta {
 namespace {
 
-constexpr int kWarps = 4, kThreads = 32 * kWarps, kKeys = 16, kR = 8;
+constexpr int kWarps = 4, kThreads = 32 * kWarps, kKeys = 16, kR = kDiffGroupRows;
+constexpr int kUnit = kWarps * kKeys;       // keys of a step of a block
+constexpr int kStart = 3;                   // steps that the beginning and end of a range cost: what shares are counted in
+                                            // (32 requests of 1 to 4k keys: 95, 71, 58, 56, 56 us with 0, 1, 2, 3, 4)
 
 struct DecodeArgs {
     DiffProblem p;
     DiffPartials part;
-    int groups;                 // groups of 8 rows per KV head
     float scale_log2;
 };
 
@@ -50,8 +55,13 @@ __device__ __forceinline__ uint4 load16(const __nv_bfloat16 *p, bool in) {
 }
 __device__ __forceinline__ uint32_t word(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
+// a / b of positive numbers, in 32 bits where they are small (a 64-bit division takes 100 cycles)
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+    return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 template <int D>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2)
 diff_decode_kernel(const __grid_constant__ DecodeArgs a) {
     constexpr int kSeg = D / 32;          // 64-byte pieces of a row; the first half of them is map 1
     constexpr int kCh = D / 64;           // 16-byte pieces of a V row per lane
@@ -61,184 +71,246 @@ diff_decode_kernel(const __grid_constant__ DecodeArgs a) {
     const DiffProblem &p = a.p;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
     const int gq = p.H / p.H_kv, rows = gq * p.Nq;
-    const int split = (int)(blockIdx.x % a.part.splits);
-    int rest = (int)(blockIdx.x / a.part.splits);
-    const int r0 = (rest % a.groups) * kR; rest /= a.groups;
-    const int hk = rest % p.H_kv, b = rest / p.H_kv;
-    const DiffSpan sp = diff_span(p.q_lens, p.kv_lens, b, p.Nq, p.Nk);
-    const int per = ((sp.kl + a.part.splits - 1) / a.part.splits + kKeys - 1) / kKeys * kKeys;
-    const long long lo64 = (long long)split * per;
-    const int u_lo = (int)min(lo64, (long long)sp.kl);
-    // keys the two rows of this lane see (columns 2 c, 2 c + 1 of S^T), and the most any row sees
-    auto keys_of = [&](int r) { return r0 + r < rows ? sp.keys((r0 + r) % p.Nq, p.causal) : 0; };
-    const int k0 = keys_of(2 * c), k1 = keys_of(2 * c + 1);
-    int most = max(k0, k1);
-    most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
-    most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-    const int end = (int)min(min(lo64 + per, (long long)sp.kl), (long long)most);
-
-    // Q: row g of the group, this lane's 16 bytes of every piece
-    uint4 q[kSeg];
-    {
-        const int r = r0 + g, h = hk * gq + r / p.Nq, t = r % p.Nq;
-        const bool in = r < rows && t < sp.ql;
-        const __nv_bfloat16 *row = (const __nv_bfloat16 *)p.q + b * p.sq.b + h * p.sq.h + (long long)t * p.sq.n + 8 * c;
-#pragma unroll
-        for (int s = 0; s < kSeg; ++s) q[s] = load16(row + 32 * s, in);
-    }
-    const __nv_bfloat16 *kb = (const __nv_bfloat16 *)p.k + b * p.sk.b + hk * p.sk.h + 8 * c;
-    const __nv_bfloat16 *vb = (const __nv_bfloat16 *)p.v + b * p.sv.b + hk * p.sv.h + 8 * g;
-    uint4 kr[2][kSeg], vr[4][kCh];
-    // keys g and g + 8 of a step; keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9
-    auto load_k = [&](int u) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int x = u + g + 8 * i;
-#pragma unroll
-            for (int s = 0; s < kSeg; ++s) kr[i][s] = load16(kb + (long long)x * p.sk.n + 32 * s, x < end);
-        }
+    // This block's share: units [x, x_end) of all pairs' units, pair after pair: kStart units without keys, then the units of 64
+    // keys.
+    const int per_entry = p.H_kv * a.part.groups;
+    auto units_of = [&](int i) {
+        const int kl = diff_span(p.q_lens, p.kv_lens, i, p.Nq, p.Nk).kl;
+        return kl > 0 ? (kl + kUnit - 1) / kUnit + kStart : 0;
     };
-    auto load_v = [&](int u) {
+    long long all = 0;
+    if (p.kv_lens) {
+        for (int i = lane; i < p.B; i += 32) all += units_of(i);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int x = u + 2 * c + (i & 1) + 8 * (i >> 1);
+        for (int w = 16; w > 0; w >>= 1) all += __shfl_xor_sync(0xffffffffu, all, w);
+    } else {
+        all = (long long)p.B * units_of(0);
+    }
+    all *= per_entry;
+    // (two units or more: a range has no empty share between its own)
+    const int share = (int)blockIdx.x, shares = (int)min((long long)a.part.shares, (all + 1) / 2);
+    if (share >= shares) return;
+    long long x = quotient(share * all, shares);
+    const long long x_end = quotient((share + 1ll) * all, shares);
+    // the entry b that unit x falls into, and the units `before` it
+    int b = 0, units = 0;
+    long long before = 0;
+    if (p.kv_lens) {
+        for (int i0 = 0;; i0 += 32) {
+            const int n = i0 + lane < p.B ? units_of(i0 + lane) : 0;
+            long long upto = n;
 #pragma unroll
-            for (int s = 0; s < kCh; ++s) vr[i][s] = load16(vb + (long long)x * p.sv.n + 64 * s, x < end);
+            for (int w = 1; w < 32; w <<= 1) {
+                const long long y = __shfl_up_sync(0xffffffffu, upto, w);
+                if (lane >= w) upto += y;
+            }
+            const unsigned beyond = __ballot_sync(0xffffffffu, before + upto * per_entry > x);
+            if (beyond || i0 + 32 >= p.B) {
+                const int l = beyond ? __ffs(beyond) - 1 : 31;           // (there always is one)
+                b = i0 + l;
+                units = __shfl_sync(0xffffffffu, n, l);
+                before += (__shfl_sync(0xffffffffu, upto, l) - units) * per_entry;
+                break;
+            }
+            before += __shfl_sync(0xffffffffu, upto, 31) * per_entry;
         }
-    };
+    } else {
+        units = units_of(0);
+        b = (int)quotient(x, (long long)units * per_entry);
+        before = (long long)b * units * per_entry;
+    }
+    int of = (int)quotient(x - before, units);
+    before += (long long)of * units;
+    while (x < x_end) {
+        const int u_first = (int)(x - before), u_last = (int)min((long long)units, x_end - before);
+        const int hk = of / a.part.groups, r0 = of % a.part.groups * kR;
+        const int slot0 = share + b * per_entry + of;         // grows from range to range: of a share, or of a pair
+        if (u_first == 0 && tid == 0) {
+            const int last = (int)quotient((before + units) * shares - 1, all);   // share of the pair's last unit
+            a.part.first[b * per_entry + of] = make_int2(slot0, last - share + 1);
+        }
+        const DiffSpan sp = diff_span(p.q_lens, p.kv_lens, b, p.Nq, p.Nk);
+        const int u_lo = max(u_first - kStart, 0) * kUnit;
+        // keys the two rows of this lane see (columns 2 c, 2 c + 1 of S^T), and the most any row sees
+        auto keys_of = [&](int r) { return r0 + r < rows ? sp.keys((r0 + r) % p.Nq, p.causal) : 0; };
+        const int k0 = keys_of(2 * c), k1 = keys_of(2 * c + 1);
+        int most = max(k0, k1);
+        most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+        most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+        const int end = (int)min(min((long long)max(u_last - kStart, 0) * kUnit, (long long)sp.kl), (long long)most);
 
-    float o[2][kMt][4];
+        // Q: row g of the group, this lane's 16 bytes of every piece
+        uint4 q[kSeg];
+        {
+            const int r = r0 + g, h = hk * gq + r / p.Nq, t = r % p.Nq;
+            const bool in = r < rows && t < sp.ql;
+            const __nv_bfloat16 *row = (const __nv_bfloat16 *)p.q + b * p.sq.b + h * p.sq.h + (long long)t * p.sq.n + 8 * c;
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int i = 0; i < kMt; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[m][i][e] = 0.f;
-    float ref[2][2], l[2][2];             // [map][row 2 c, 2 c + 1]; ref is the same in the 8 lanes of a row
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            ref[m][e] = -INFINITY;
-            l[m][e] = 0.f;
+            for (int s = 0; s < kSeg; ++s) q[s] = load16(row + 32 * s, in);
         }
-    int u = u_lo + warp * kKeys;
-    if (u < end) {
-        load_k(u);
-        load_v(u);
-    }
-    for (; u < end; u += kWarps * kKeys) {
-        float s[2][4];
+        const __nv_bfloat16 *kb = (const __nv_bfloat16 *)p.k + b * p.sk.b + hk * p.sk.h + 8 * c;
+        const __nv_bfloat16 *vb = (const __nv_bfloat16 *)p.v + b * p.sv.b + hk * p.sv.h + 8 * g;
+        uint4 kr[2][kSeg], vr[4][kCh];
+        // keys g and g + 8 of a step; keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9
+        auto load_k = [&](int u) {
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
+            for (int i = 0; i < 2; ++i) {
+                const int x = u + g + 8 * i;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[m][e] = 0.f;
-#pragma unroll
-            for (int i = 0; i < kSeg / 2; ++i) {
-                const int x = m * (kSeg / 2) + i;
-                mma16816(s[m], kr[0][x].x, kr[1][x].x, kr[0][x].y, kr[1][x].y, q[x].x, q[x].y);
-                mma16816(s[m], kr[0][x].z, kr[1][x].z, kr[0][x].w, kr[1][x].w, q[x].z, q[x].w);
+                for (int s = 0; s < kSeg; ++s) kr[i][s] = load16(kb + (long long)x * p.sk.n + 32 * s, x < end);
             }
-        }
-        load_k(u + kWarps * kKeys);       // (keys from `end` on are zeros, without a load)
-        uint32_t hi[2][2], lo[2][2];
+        };
+        auto load_v = [&](int u) {
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
+            for (int i = 0; i < 4; ++i) {
+                const int x = u + 2 * c + (i & 1) + 8 * (i >> 1);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int key = u + g + 8 * (e >> 1);
-                s[m][e] = key < ((e & 1) ? k1 : k0) ? s[m][e] * a.scale_log2 : -INFINITY;
+                for (int s = 0; s < kCh; ++s) vr[i][s] = load16(vb + (long long)x * p.sv.n + 64 * s, x < end);
             }
-            const float m0 = fmaxf(s[m][0], s[m][2]), m1 = fmaxf(s[m][1], s[m][3]);
-            if (__any_sync(0xffffffffu, m0 > ref[m][0] + 8.f || m1 > ref[m][1] + 8.f)) {
-                float n0 = m0, n1 = m1;
+        };
+
+        float o[2][kMt][4];
 #pragma unroll
-                for (int w = 4; w < 32; w <<= 1) {
-                    n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, w));
-                    n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, w));
-                }
-                n0 = fmaxf(n0, ref[m][0]);
-                n1 = fmaxf(n1, ref[m][1]);
-                const float f0 = ref[m][0] == -INFINITY ? 0.f : fast_exp2(ref[m][0] - n0);
-                const float f1 = ref[m][1] == -INFINITY ? 0.f : fast_exp2(ref[m][1] - n1);
-                ref[m][0] = n0;
-                ref[m][1] = n1;
-                l[m][0] *= f0;
-                l[m][1] *= f1;
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int i = 0; i < kMt; ++i) {
-                    o[m][i][0] *= f0; o[m][i][1] *= f1; o[m][i][2] *= f0; o[m][i][3] *= f1;
-                }
-            }
-            const float z0 = ref[m][0] == -INFINITY ? 0.f : ref[m][0], z1 = ref[m][1] == -INFINITY ? 0.f : ref[m][1];
-            const float p0 = fast_exp2(s[m][0] - z0), p1 = fast_exp2(s[m][1] - z1);
-            const float p2 = fast_exp2(s[m][2] - z0), p3 = fast_exp2(s[m][3] - z1);
-            l[m][0] += p0 + p2;
-            l[m][1] += p1 + p3;
-            const uint32_t h0 = pack_bf16x2(p0, p1), h1 = pack_bf16x2(p2, p3);
-            hi[m][0] = turn8x8(h0);
-            hi[m][1] = turn8x8(h1);
-            lo[m][0] = turn8x8(pack_bf16x2(p0 - __uint_as_float(h0 << 16), p1 - __uint_as_float(h0 & 0xFFFF0000u)));
-            lo[m][1] = turn8x8(pack_bf16x2(p2 - __uint_as_float(h1 << 16), p3 - __uint_as_float(h1 & 0xFFFF0000u)));
-        }
+            for (int i = 0; i < kMt; ++i)
 #pragma unroll
-        for (int i = 0; i < kMt; ++i) {
-            // features 64 (i / 4) + 8 g + 2 (i % 4) (tile rows 0 .. 7) and the next (rows 8 .. 15)
-            const uint32_t w0 = word(vr[0][i / 4], i % 4), w1 = word(vr[1][i / 4], i % 4);
-            const uint32_t w2 = word(vr[2][i / 4], i % 4), w3 = word(vr[3][i / 4], i % 4);
-            const uint32_t a0 = __byte_perm(w0, w1, 0x5410), a1 = __byte_perm(w0, w1, 0x7632);
-            const uint32_t a2 = __byte_perm(w2, w3, 0x5410), a3 = __byte_perm(w2, w3, 0x7632);
-#pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                mma16816(o[m][i], a0, a1, a2, a3, hi[m][0], hi[m][1]);
-                mma16816(o[m][i], a0, a1, a2, a3, lo[m][0], lo[m][1]);
-            }
-        }
-        load_v(u + kWarps * kKeys);
-    }
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-            for (int w = 4; w < 32; w <<= 1) l[m][e] += __shfl_xor_sync(0xffffffffu, l[m][e], w);
-    if (g == 0)
+                for (int e = 0; e < 4; ++e) o[m][i][e] = 0.f;
+        float ref[2][2], l[2][2];             // [map][row 2 c, 2 c + 1]; ref is the same in the 8 lanes of a row
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                s_ml[warp][m][0][2 * c + e] = ref[m][e];
-                s_ml[warp][m][1][2 * c + e] = l[m][e];
+                ref[m][e] = -INFINITY;
+                l[m][e] = 0.f;
+            }
+        int u = u_lo + warp * kKeys;
+        if (u < end) {
+            load_k(u);
+            load_v(u);
+        }
+        for (; u < end; u += kWarps * kKeys) {
+            float s[2][4];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[m][e] = 0.f;
+#pragma unroll
+                for (int i = 0; i < kSeg / 2; ++i) {
+                    const int x = m * (kSeg / 2) + i;
+                    mma16816(s[m], kr[0][x].x, kr[1][x].x, kr[0][x].y, kr[1][x].y, q[x].x, q[x].y);
+                    mma16816(s[m], kr[0][x].z, kr[1][x].z, kr[0][x].w, kr[1][x].w, q[x].z, q[x].w);
+                }
+            }
+            load_k(u + kWarps * kKeys);       // (keys from `end` on are zeros, without a load)
+            uint32_t hi[2][2], lo[2][2];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int key = u + g + 8 * (e >> 1);
+                    s[m][e] = key < ((e & 1) ? k1 : k0) ? s[m][e] * a.scale_log2 : -INFINITY;
+                }
+                const float m0 = fmaxf(s[m][0], s[m][2]), m1 = fmaxf(s[m][1], s[m][3]);
+                if (__any_sync(0xffffffffu, m0 > ref[m][0] + 8.f || m1 > ref[m][1] + 8.f)) {
+                    float n0 = m0, n1 = m1;
+#pragma unroll
+                    for (int w = 4; w < 32; w <<= 1) {
+                        n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, w));
+                        n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, w));
+                    }
+                    n0 = fmaxf(n0, ref[m][0]);
+                    n1 = fmaxf(n1, ref[m][1]);
+                    const float f0 = ref[m][0] == -INFINITY ? 0.f : fast_exp2(ref[m][0] - n0);
+                    const float f1 = ref[m][1] == -INFINITY ? 0.f : fast_exp2(ref[m][1] - n1);
+                    ref[m][0] = n0;
+                    ref[m][1] = n1;
+                    l[m][0] *= f0;
+                    l[m][1] *= f1;
+#pragma unroll
+                    for (int i = 0; i < kMt; ++i) {
+                        o[m][i][0] *= f0; o[m][i][1] *= f1; o[m][i][2] *= f0; o[m][i][3] *= f1;
+                    }
+                }
+                const float z0 = ref[m][0] == -INFINITY ? 0.f : ref[m][0], z1 = ref[m][1] == -INFINITY ? 0.f : ref[m][1];
+                const float p0 = fast_exp2(s[m][0] - z0), p1 = fast_exp2(s[m][1] - z1);
+                const float p2 = fast_exp2(s[m][2] - z0), p3 = fast_exp2(s[m][3] - z1);
+                l[m][0] += p0 + p2;
+                l[m][1] += p1 + p3;
+                const uint32_t h0 = pack_bf16x2(p0, p1), h1 = pack_bf16x2(p2, p3);
+                hi[m][0] = turn8x8(h0);
+                hi[m][1] = turn8x8(h1);
+                lo[m][0] = turn8x8(pack_bf16x2(p0 - __uint_as_float(h0 << 16), p1 - __uint_as_float(h0 & 0xFFFF0000u)));
+                lo[m][1] = turn8x8(pack_bf16x2(p2 - __uint_as_float(h1 << 16), p3 - __uint_as_float(h1 & 0xFFFF0000u)));
             }
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+            for (int i = 0; i < kMt; ++i) {
+                // features 64 (i / 4) + 8 g + 2 (i % 4) (tile rows 0 .. 7) and the next (rows 8 .. 15)
+                const uint32_t w0 = word(vr[0][i / 4], i % 4), w1 = word(vr[1][i / 4], i % 4);
+                const uint32_t w2 = word(vr[2][i / 4], i % 4), w3 = word(vr[3][i / 4], i % 4);
+                const uint32_t a0 = __byte_perm(w0, w1, 0x5410), a1 = __byte_perm(w0, w1, 0x7632);
+                const uint32_t a2 = __byte_perm(w2, w3, 0x5410), a3 = __byte_perm(w2, w3, 0x7632);
 #pragma unroll
-        for (int i = 0; i < kMt; ++i) {
-            const int f = 64 * (i / 4) + 8 * g + 2 * (i % 4);
-            float *x = s_o + ((warp * 2 + m) * kR + 2 * c) * D + f;
-            *(float2 *)x = make_float2(o[m][i][0], o[m][i][2]);
-            *(float2 *)(x + D) = make_float2(o[m][i][1], o[m][i][3]);
+                for (int m = 0; m < 2; ++m) {
+                    mma16816(o[m][i], a0, a1, a2, a3, hi[m][0], hi[m][1]);
+                    mma16816(o[m][i], a0, a1, a2, a3, lo[m][0], lo[m][1]);
+                }
+            }
+            load_v(u + kWarps * kKeys);
         }
-    __syncthreads();
-    // the block's sums of every (row, map): scaled to the largest of its warps' references
-    for (int i = tid; i < kR * 2 * D; i += kThreads) {
-        const int f = i % D, m = (i / D) & 1, r = i / (2 * D);
-        if (r0 + r >= rows) break;
-        const int h = hk * gq + (r0 + r) / p.Nq, t = (r0 + r) % p.Nq;
-        float mx = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, s_ml[w][m][0][r]);
-        const float z = mx == -INFINITY ? 0.f : mx;
-        float sum = 0.f, x = 0.f;
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            const float e = fast_exp2(s_ml[w][m][0][r] - z);
-            sum = fmaf(s_ml[w][m][1][r], e, sum);
-            x = fmaf(s_o[((w * 2 + m) * kR + r) * D + f], e, x);
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int w = 4; w < 32; w <<= 1) l[m][e] += __shfl_xor_sync(0xffffffffu, l[m][e], w);
+        if (g == 0)
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    s_ml[warp][m][0][2 * c + e] = ref[m][e];
+                    s_ml[warp][m][1][2 * c + e] = l[m][e];
+                }
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int i = 0; i < kMt; ++i) {
+                const int f = 64 * (i / 4) + 8 * g + 2 * (i % 4);
+                float *x = s_o + ((warp * 2 + m) * kR + 2 * c) * D + f;
+                *(float2 *)x = make_float2(o[m][i][0], o[m][i][2]);
+                *(float2 *)(x + D) = make_float2(o[m][i][1], o[m][i][3]);
+            }
+        __syncthreads();
+        // the block's sums of every (row, map): scaled to the largest of its warps' references
+        for (int i = tid; i < kR * 2 * D; i += kThreads) {
+            const int f = i % D, m = (i / D) & 1, r = i / (2 * D);
+            if (r0 + r >= rows) break;
+            float mx = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, s_ml[w][m][0][r]);
+            const float z = mx == -INFINITY ? 0.f : mx;
+            float sum = 0.f, v = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float e = fast_exp2(s_ml[w][m][0][r] - z);
+                sum = fmaf(s_ml[w][m][1][r], e, sum);
+                v = fmaf(s_o[((w * 2 + m) * kR + r) * D + f], e, v);
+            }
+            const long long slot = (long long)slot0 * a.part.rows_per_slot + r;
+            a.part.acc[slot * 2 * D + m * D + f] = v;
+            if (f == 0) *(float2 *)((float *)(a.part.ml + slot) + 2 * m) = make_float2(mx, sum);
         }
-        const long long slot = (((long long)b * p.H + h) * p.Nq + t) * a.part.splits + split;
-        a.part.acc[slot * 2 * D + m * D + f] = x;
-        if (f == 0) *(float2 *)((float *)(a.part.ml + slot) + 2 * m) = make_float2(mx, sum);
+        // the next pair that has keys
+        x = before + u_last;
+        if (x == x_end) break;
+        before = x;
+        if (++of == per_entry) {
+            of = 0;
+            do units = units_of(++b);
+            while (units == 0);
+        }
+        __syncthreads();                      // (the sums have been read)
     }
 }
 
@@ -247,12 +319,8 @@ int launch_d(const DiffProblem &p, const DiffPartials &part) {
     DecodeArgs a = {};
     a.p = p;
     a.part = part;
-    const long long rows = (long long)(p.H / p.H_kv) * p.Nq;
-    a.groups = (int)((rows + kR - 1) / kR);
     a.scale_log2 = p.scale * 1.4426950408889634f;
-    const long long blocks = (long long)p.B * p.H_kv * a.groups * part.splits;
-    if (blocks > 0x7FFFFFFFll) return TA_ERR_TOO_LARGE;
-    return launch_kernel(diff_decode_kernel<D>, (unsigned)blocks, kThreads, kWarps * 2 * kR * D * sizeof(float), p.stream, false, a);
+    return launch_kernel(diff_decode_kernel<D>, (unsigned)part.shares, kThreads, kWarps * 2 * kR * D * sizeof(float), p.stream, false, a);
 }
 
 }  // namespace

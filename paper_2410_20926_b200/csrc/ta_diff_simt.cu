@@ -495,11 +495,21 @@ diff_combine_kernel(const __grid_constant__ SimtArgs a) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int t = (int)(row % p.Nq);
     const int bh = (int)(row / p.Nq), b = bh / p.H, h = bh - b * p.H;
-    const int ns = a.part.splits, D = p.D;
-    const float4 *ml = a.part.ml + row * ns;
+    const int D = p.D;
+    int ns = a.part.splits, step = 1;                  // slots of the row's ranges
+    long long from = row * ns;
+    if (a.part.first) {
+        const int gq = p.H / p.H_kv, r = h % gq * p.Nq + t;
+        const int pair = (b * p.H_kv + h / gq) * a.part.groups + r / kDiffGroupRows;
+        const int2 f = diff_span(p.q_lens, p.kv_lens, b, p.Nq, p.Nk).kl > 0 ? a.part.first[pair] : make_int2(0, 0);
+        ns = f.y;
+        step = a.part.rows_per_slot;
+        from = (long long)f.x * step + r % kDiffGroupRows;
+    }
+    const float4 *ml = a.part.ml + from;
     float m1 = -INFINITY, m2 = -INFINITY;
     for (int s = lane; s < ns; s += 32) {
-        const float4 x = ml[s];
+        const float4 x = ml[(long long)s * step];
         m1 = fmaxf(m1, x.x);
         m2 = fmaxf(m2, x.z);
     }
@@ -517,11 +527,11 @@ diff_combine_kernel(const __grid_constant__ SimtArgs a) {
         for (int i = 0; i < 4; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
         for (int s = warp; s < ns; s += kJoinWarps) {
-            const float4 x = ml[s];
+            const float4 x = ml[(long long)s * step];
             const float w1 = exp2f(x.x - m1), w2 = exp2f(x.z - m2);
             l1 = fmaf(x.y, w1, l1);
             l2 = fmaf(x.w, w2, l2);
-            const float4 *o = reinterpret_cast<const float4 *>(a.part.acc + (row * ns + s) * 2 * D);
+            const float4 *o = reinterpret_cast<const float4 *>(a.part.acc + (from + (long long)s * step) * 2 * D);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int c = lane + 32 * i;
@@ -543,12 +553,12 @@ diff_combine_kernel(const __grid_constant__ SimtArgs a) {
         for (int c = lane; c < 2 * D; c += 32) {
             float x = 0.f;
             for (int s = warp; any && s < ns; s += kJoinWarps)
-                x = fmaf(a.part.acc[(row * ns + s) * 2 * D + c], c < D ? exp2f(ml[s].x - m1) : exp2f(ml[s].z - m2), x);
+                x = fmaf(a.part.acc[(from + (long long)s * step) * 2 * D + c], c < D ? exp2f(ml[(long long)s * step].x - m1) : exp2f(ml[(long long)s * step].z - m2), x);
             s_acc[warp][c] = x;
         }
         for (int s = warp; any && s < ns; s += kJoinWarps) {
-            l1 = fmaf(ml[s].y, exp2f(ml[s].x - m1), l1);
-            l2 = fmaf(ml[s].w, exp2f(ml[s].z - m2), l2);
+            l1 = fmaf(ml[(long long)s * step].y, exp2f(ml[(long long)s * step].x - m1), l1);
+            l2 = fmaf(ml[(long long)s * step].w, exp2f(ml[(long long)s * step].z - m2), l2);
         }
     }
     if (lane == 0) {

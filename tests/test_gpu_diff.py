@@ -350,6 +350,16 @@ def test_key_ranges_of_few_rows(shape):
     check(*shape, grad=False, kl=[Nk - 37 * i % Nk for i in range(B)])
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_requests_of_all_lengths(D):
+    """More entries than a warp's lanes, with empty ones first, last and in a row."""
+    gen = np.random.default_rng(5)
+    kl = [0] * 35 + [int(x) for x in gen.integers(0, 700, 60)] + [700, 1, 0, 64, 65, 0]
+    check(len(kl), 4, 2, 1, 700, D, grad=False, kl=kl)
+    check(len(kl), 8, 1, 3, 700, D, grad=False, kl=kl, ql=[(7 * i) % 4 for i in range(len(kl))])
+    check(3, 4, 2, 1, 700, D, grad=False, kl=[0, 0, 0])
+
+
 @pytest.mark.parametrize("dtype,D", [("bfloat16", 128), ("float32", 64)])
 def test_offsets_beyond_32_bits(dtype, D):
     """Tokens 2^20 elements apart: the last of 2100 stand behind element 2^31."""
