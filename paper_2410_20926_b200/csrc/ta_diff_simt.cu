@@ -378,7 +378,13 @@ template <int R>
 __device__ __forceinline__ void read_rows(const float *src, float (&x)[R]) {
     if constexpr (R % 4 == 0) {
 #pragma unroll
-        for (int r = 0; r < R; r += 4) *reinterpret_cast<float4 *>(x + r) = *reinterpret_cast<const float4 *>(src + r);
+        for (int r = 0; r < R; r += 4) {
+            const float4 v = *reinterpret_cast<const float4 *>(src + r);
+            x[r] = v.x;
+            x[r + 1] = v.y;
+            x[r + 2] = v.z;
+            x[r + 3] = v.w;
+        }
     } else {
 #pragma unroll
         for (int r = 0; r < R; ++r) x[r] = src[r];
