@@ -395,8 +395,8 @@ int ta_rotary(const ta_rotary_params *p);
  * kv_lens[b] on, and in q and dout from q_lens[b] on, does not matter (NaN included).
  *
  * bf16 with D = 64 or 128 and 16-byte aligned rows runs on the tensor cores (scores and sums in fp32, weights rounded to
- * bf16 before the value product); with few query rows (Nq * H / H_kv <= 32) on a kernel that splits the keys over
- * the GPU.  Everything else -- fp32 (fp32 arithmetic throughout), other even D up to 256, unaligned views,
+ * bf16 before the value product); with few query rows (Nq * H / H_kv <= 32, or few in all against thousands of keys)
+ * on a kernel that splits the keys over the GPU.  Everything else -- fp32 (fp32 arithmetic throughout), other even D up to 256, unaligned views,
  * TA_FLAG_NO_TENSOR_CORE -- runs on CUDA-core kernels.  No atomics: results repeat bit for bit.  (How the keys of few rows are
  * shared out depends on the whole batch, so an entry's last bits may differ between batches.)
  */

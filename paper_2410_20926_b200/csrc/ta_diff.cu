@@ -28,6 +28,13 @@ int check_shape(int B, int H, int H_kv, int Nq, int Nk, int D, int dtype) {
 bool few_rows(int H, int H_kv, int Nq) { return (long long)(H / H_kv) * Nq <= kSplitRows; }
 
 long long row_groups(int H, int H_kv, int Nq) { return ((long long)(H / H_kv) * Nq + kDiffGroupRows - 1) / kDiffGroupRows; }
+// On the tensor cores, so few rows in all that tiles of 128 leave most of the GPU idle, against many keys (a chunk of a prompt
+// behind a cache): groups of 8 rows with the keys split are faster, up to twice as many at head dim 64.  64 rows, 8 heads on 2
+// (64 groups), D=128, 16k keys: 69 us, in tiles 211 us; 4k keys 28 and 57 us; 1k keys 19 and 18 us.  128 groups, 4k keys: 47 and
+// 73 us; 256 groups 82 and 54 us (D=64: 48 and 54 us).
+bool few_tiles(int B, int H, int H_kv, int Nq, int Nk, int D) {
+    return Nk >= 2048 && (long long)B * H_kv * row_groups(H, H_kv, Nq) * D <= 16384;
+}
 // Key ranges of the CUDA-core split kernel: six blocks per SM, ranges of 256 keys or more.
 int num_splits(int B, int H, int H_kv, int Nq, int Nk) {
     const long long blocks = (long long)B * H_kv * row_groups(H, H_kv, Nq);
@@ -86,10 +93,11 @@ struct ForwardLayout {
 };
 ForwardLayout forward_layout(int B, int H, int H_kv, int Nq, int Nk, int D) {
     ForwardLayout L = {};
-    if (!few_rows(H, H_kv, Nq)) return L;
+    const bool rows_few = few_rows(H, H_kv, Nq);
+    if (!rows_few && !few_tiles(B, H, H_kv, Nq, Nk, D)) return L;
     const size_t rows = (size_t)(H / H_kv) * Nq, pairs = (size_t)B * H_kv * row_groups(H, H_kv, Nq);
     L.rows_per_slot = (int)(rows < (size_t)kDiffGroupRows ? rows : (size_t)kDiffGroupRows);
-    size_t slots = (size_t)B * H * Nq * num_splits(B, H, H_kv, Nq, Nk);
+    size_t slots = rows_few ? (size_t)B * H * Nq * num_splits(B, H, H_kv, Nq, Nk) : 0;
     const size_t shared = (pairs + num_shares(B, H, H_kv, Nq, Nk, D)) * L.rows_per_slot;
     if (shared > slots) slots = shared;
     L.acc = up256(slots * sizeof(float4));
@@ -215,7 +223,8 @@ int forward_impl(const ta_diff_params &p) {
     const bool tc = tc_shape(d.D, d.dtype, d.scale, p.flags) && tma_ok(d.q, d.sq, d.B, d.H, d.Nq) &&
                     tma_ok(d.k, d.sk, d.B, d.H_kv, d.Nk) && tma_ok(d.v, d.sv, d.B, d.H_kv, d.Nk) &&
                     tma_ok(d.out, d.so, d.B, d.H, d.Nq);
-    if (!few_rows(p.H, p.H_kv, p.Nq)) return tc ? launch_diff_tc(d) : launch_diff_simt(d);
+    if (!few_rows(p.H, p.H_kv, p.Nq) && !(tc && few_tiles(p.B, p.H, p.H_kv, p.Nq, p.Nk, p.D)))
+        return tc ? launch_diff_tc(d) : launch_diff_simt(d);
     char *ws = (char *)p.workspace;
     PooledGuard pooled{nullptr, d.stream};
     if (!ws) {

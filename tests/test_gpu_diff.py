@@ -350,6 +350,17 @@ def test_key_ranges_of_few_rows(shape):
     check(*shape, grad=False, kl=[Nk - 37 * i % Nk for i in range(B)])
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+def test_chunk_behind_a_long_cache(D, causal):
+    """Rows too few for tiles against many keys; just below and above where that begins."""
+    check(1, 8, 2, 64, 2100, D, causal=causal)
+    check(2, 4, 4, 43, 2048, D, causal=causal, ql=[43, 17], kl=[2048, 30])
+    check(1, 2, 1, 130, 2300, D, causal=causal, ql=[129], kl=[2299])
+    check(1, 8, 1, 70, 2047, D, causal=causal, grad=False)
+    check(1, 8, 2, 257, 2100, D, causal=causal, grad=False)
+
+
 @pytest.mark.parametrize("D", [64, 128])
 def test_many_requests_of_all_lengths(D):
     """More entries than a warp's lanes, with empty ones first, last and in a row."""
