@@ -112,6 +112,11 @@ def _on(device):
     return _SAME_DEVICE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
 
 
+def _grad_enabled():
+    import torch
+    return torch.is_grad_enabled()
+
+
 def _strided(t):
     """(tensor, its three outer strides); a contiguous copy where the innermost features are not adjacent."""
     b, h, n, d = t.stride()
@@ -206,7 +211,7 @@ def multi_axis_rotary(q, k, sections, positions=None, dims=None, token_offset=0,
     dims = None if dims is None else [int(x) for x in dims]
     _check_rotary(q, k, sections, positions, dims)
     args = (sections, dims, int(token_offset), float(base), int(parts), bool(interleaved), bool(per_axis_ladder))
-    if not q.requires_grad and (k is None or not k.requires_grad):
+    if not _grad_enabled() or not (q.requires_grad or (k is not None and k.requires_grad)):
         return _rotary_call(q, k, sections, positions, *args[1:], False)
     if _ROTARY is None:
         _ROTARY = _rotary_function()
@@ -304,10 +309,13 @@ def differential_attention(q, k, v, lam, causal=True, softmax_scale=None, q_lens
     s: 1/sqrt(D/2) unless given.  The query rows stand at the end of the keys: row t has position
     kv_lens[b] - q_lens[b] + t and, with `causal`, sees the keys up to it; q_lens, kv_lens: int32 CUDA tensors [B] of
     valid rows and keys (all of them by default).  Rows that see nothing are 0.  Returns [B, H, Nq, D], contiguous.
+
+    Both passes may be captured into a CUDA graph; as for every torch function, no autograd graph of the same leaves that
+    was built on another stream may be alive while a backward pass is captured.
     """
     global _DIFF
     _check_diff(q, k, v, lam, q_lens, kv_lens)
-    if not (q.requires_grad or k.requires_grad or v.requires_grad or lam.requires_grad):
+    if not _grad_enabled() or not (q.requires_grad or k.requires_grad or v.requires_grad or lam.requires_grad):
         return _diff_forward(q, k, v, lam.contiguous(), bool(causal), softmax_scale, q_lens, kv_lens, False)[0]
     if _DIFF is None:
         _DIFF = _diff_function()

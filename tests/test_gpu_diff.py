@@ -409,3 +409,17 @@ def test_second_derivatives_are_refused():
     dq, = torch.autograd.grad(out.float().square().sum(), q, create_graph=True)
     with pytest.raises(RuntimeError):
         dq.float().sum().backward()
+
+
+def test_nothing_is_saved_without_gradients(monkeypatch):
+    """Serving with a learned lambda: under no_grad the call is the plain one, and its result the same."""
+    import torch
+    from paper_2410_20926_b200 import autograd
+    q, k, v = draw(90, (1, 4, 40, 64), (1, 2, 40, 64), (1, 2, 40, 64))
+    lam = lambdas(91, 4).requires_grad_()
+    seen, plain = [], autograd._diff_forward
+    monkeypatch.setattr(autograd, "_diff_forward", lambda *a: seen.append(a[-1]) or plain(*a))
+    want = ta.differential_attention(q, k, v, lam)
+    with torch.no_grad():
+        got = ta.differential_attention(q, k, v, lam)
+    assert seen == [True, False] and want.requires_grad and not got.requires_grad and torch.equal(got, want)
