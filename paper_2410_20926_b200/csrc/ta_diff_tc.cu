@@ -54,13 +54,14 @@ struct Cfg {
     static constexpr uint32_t kOffBar = kOffV + kNKV * kHTile;
     static constexpr int kNumBars = 2 * kNQ + 2 * kNKV + 4 + 4 + 2 + 3;
     static constexpr uint32_t kOffX = kOffBar + ((kNumBars * 8 + 16 + 15) & ~15);      // 1 / l of both maps, 128 rows
-    static constexpr uint32_t kSmem = kOffX + 2 * kRows * 4 + 1024;
+    static constexpr uint32_t kOffDeal = kOffX + 2 * kRows * 4;
+    static constexpr uint32_t kSmem = kOffDeal + kDealt * 4 + 1024;
     static constexpr uint32_t kColO = 256;
 };
 
 struct TcArgs {
     int B, H, H_kv, g, Nq, Nk, causal;
-    int qtiles, tile_major;
+    int qtiles, tile_major, deal;
     int total_items;
     float scale_log2;
     const int *q_lens, *kv_lens;
@@ -146,6 +147,11 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    int *dealt = (int *)(smem + C::kOffDeal);
+    if (a.deal)
+        deal_items(dealt, a.q_lens, a.kv_lens, a.B, a.H, a.Nq, a.Nk, a.qtiles, a.causal, a.total_items, warp, kThreads / 32);
+    auto item_at = [&](int round) { return a.deal ? dealt[round] : item_of_round(a.total_items, round); };
+    __syncwarp();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -159,7 +165,7 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             Armed armed;
             bool ok = true;
             for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
-                const int item = item_of_round(a.total_items, round);
+                const int item = item_at(round);
                 if (item < 0) continue;
                 const Item c = decode(a, item);
                 if (c.n == 0) continue;
@@ -190,7 +196,7 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             uint32_t par = 0, oph = 1;               // bit p: phase of the weights in slot p; phase of o_free to wait for
             bool ok = true;
             for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
-                const int item = item_of_round(a.total_items, round);
+                const int item = item_at(round);
                 if (item < 0) continue;
                 const Item c = decode(a, item);
                 if (c.n == 0) continue;
@@ -273,7 +279,7 @@ diff_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         bool ok = true;
         uint32_t ic = 0, sc = 0, par = 0;               // items, half blocks so far; bit p: phase of the scores in slot p
         for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
-            const int item = item_of_round(a.total_items, round);
+            const int item = item_at(round);
             if (item < 0) continue;
             const Item c = decode(a, item);
             const int t = c.t0 + r;
@@ -440,6 +446,8 @@ int launch_d(const DiffProblem &p) {
     if ((rc = make_strided_map(&mq, p.q, &p.sq.b, p.B, p.H, p.Nq, D, kRows)) != TA_OK) return rc;
     if ((rc = make_strided_map(&mk, p.k, &p.sk.b, p.B, p.H_kv, p.Nk, D, kHalf)) != TA_OK) return rc;
     if ((rc = make_strided_map(&mv, p.v, &p.sv.b, p.B, p.H_kv, p.Nk, D, kHalf)) != TA_OK) return rc;
+    int dev = 0;
+    const int num_sms = current_device_sms(&dev);
     TcArgs a = {};
     a.B = p.B; a.H = p.H; a.H_kv = p.H_kv; a.g = p.H / p.H_kv; a.Nq = p.Nq; a.Nk = p.Nk; a.causal = p.causal;
     a.qtiles = (p.Nq + kRows - 1) / kRows;
@@ -448,14 +456,13 @@ int launch_d(const DiffProblem &p) {
     a.total_items = (int)items;
     // K and V of all heads against the 126 MB L2
     a.tile_major = 2ull * p.B * p.H_kv * p.Nk * D * 2 <= (96ull << 20) ? 1 : 0;
+    a.deal = (p.q_lens || p.kv_lens) && p.B <= 32 && a.tile_major && a.total_items <= kDealt * num_sms ? 1 : 0;
     a.scale_log2 = p.scale * 1.4426950408889634f;
     a.q_lens = p.q_lens; a.kv_lens = p.kv_lens;
     a.lambda = p.lambda; a.lambda_count = p.lambda_count;
     a.out = (__nv_bfloat16 *)p.out;
     a.so = p.so;
     a.lse = p.lse; a.o16 = p.o16; a.ostep = p.ostep;
-    int dev = 0;
-    const int num_sms = current_device_sms(&dev);
     static PerDeviceOnce configured;
     if (!configured.is_done(dev)) {
         const cudaError_t e = cudaFuncSetAttribute(diff_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);

@@ -164,6 +164,79 @@ __device__ __forceinline__ int item_of_round(int total_items, int k) {
     return item < total_items ? item : -1;
 }
 
+// Items of a batch of different lengths (query tiles of 128 rows of B <= 32 entries), longest first and those without keys last,
+// so that dealing them forth and back evens out: in the order of a batch of one length, tiles that some entries do not
+// have leave CTAs idle.  table[k]: this CTA's k-th item, numbered (tiles - 1 - tile) * B * H + head; a warp per k, a lane per
+// entry.  (A call: inlined, the loop over the keys comes out 8 % slower.)
+constexpr int kDealt = 32;
+__device__ __noinline__ void deal_items(int *table, const int *q_lens, const int *kv_lens, int B, int H, int Nq, int Nk, int tiles,
+                                           int causal, int total, int warp, int warps) {
+    const int lane = threadIdx.x & 31, g = (int)gridDim.x, cta = (int)blockIdx.x;
+    auto sum = [](int x) {
+#pragma unroll
+        for (int w = 16; w > 0; w >>= 1) x += __shfl_xor_sync(0xffffffffu, x, w);
+        return x;
+    };
+    int mine = 0, keys = -1;                         // tiles with keys
+    if (lane < B) {
+        const DiffSpan sp = diff_span(q_lens, kv_lens, lane, Nq, Nk);
+        keys = sp.kl;
+        mine = keys > 0 ? (sp.ql + 127) >> 7 : 0;
+    }
+    const int valid = H * sum(mine);
+    int before = 0;                                  // items of entries with more keys (all keys are visible to every row)
+    if (!causal)
+        for (int o = 0; o < B; ++o) {
+            const int k = __shfl_sync(0xffffffffu, keys, o), m = __shfl_sync(0xffffffffu, mine, o);
+            if (k > keys || (k == keys && o < lane)) before += H * m;
+        }
+    const int none = lane < B ? H * (tiles - mine) : 0;
+    int none_before = none;
+#pragma unroll
+    for (int w = 1; w < 32; w <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, none_before, w);
+        if (lane >= w) none_before += x;
+    }
+    none_before -= none;
+    for (int k = warp; k < kDealt && k * g < total; k += warps) {
+        const int i = k * g + ((k & 1) ? g - 1 - cta : cta);
+        int b = 0, tile = 0, h = 0;
+        if (i >= total) {
+            if (lane == 0) table[k] = -1;
+            continue;
+        }
+        if (i >= valid) {
+            const int r = i - valid - none_before;
+            const int l = __ffs(__ballot_sync(0xffffffffu, r >= 0 && r < none)) - 1;
+            const int rl = __shfl_sync(0xffffffffu, r, l);
+            b = l;
+            tile = __shfl_sync(0xffffffffu, mine, l) + rl / H;
+            h = rl % H;
+        } else if (!causal) {
+            const int r = i - before;
+            const int l = __ffs(__ballot_sync(0xffffffffu, r >= 0 && r < H * mine)) - 1;
+            const int rl = __shfl_sync(0xffffffffu, r, l);
+            b = l;
+            tile = __shfl_sync(0xffffffffu, mine, l) - 1 - rl / H;
+            h = rl % H;
+        } else {
+            // later tiles see more: the largest x with more than i items in tiles x and up
+            int lo = 0, hi = tiles;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (H * sum(max(0, mine - mid)) > i) lo = mid; else hi = mid;
+            }
+            const int r = i - H * sum(max(0, mine - lo - 1));
+            unsigned have = __ballot_sync(0xffffffffu, mine > lo);
+            for (int j = r / H; j > 0; --j) have &= have - 1;
+            b = __ffs(have) - 1;
+            tile = lo;
+            h = r % H;
+        }
+        if (lane == 0) table[k] = (tiles - 1 - tile) * (B * H) + b * H + h;
+    }
+}
+
 // Remembers the copies a producer has started, so that they can be waited for when it gives up.
 struct Armed {
     uint32_t mask = 0, par = 0;

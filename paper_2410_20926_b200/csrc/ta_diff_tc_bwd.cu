@@ -35,6 +35,7 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
 struct BwdArgs {
     int B, H, H_kv, g, Nq, Nk, causal;
     int tiles, tile_major;         // query tiles / key blocks per head
+    int deal;                      // dQ: items dealt by their lengths
     int gi, hsplit;                // dK, dV: query heads per item, items per (key block, KV head)
     int total_items;
     long long prow;
@@ -64,7 +65,8 @@ struct DqCfg {
     static constexpr uint32_t kOffQ = 0, kOffG = kTile, kOffK = 2 * kTile, kOffV = kOffK + kNKV * kHTile;
     static constexpr uint32_t kOffBar = kOffV + kNKV * kHTile;
     static constexpr int kNumBars = 2 + 2 * kNKV + 6;
-    static constexpr uint32_t kSmem = kOffBar + kNumBars * 8 + 16 + 1024;
+    static constexpr uint32_t kOffDeal = kOffBar + kNumBars * 8 + 16;
+    static constexpr uint32_t kSmem = kOffDeal + kDealt * 4 + 1024;
     // per chain (64 keys): S_1, S_2 (dS_c over their first 32 columns), dA; then dQ
     static constexpr uint32_t kColChain = 192, kColDQ = 384;
 };
@@ -134,6 +136,11 @@ diff_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    int *dealt = (int *)(smem + C::kOffDeal);
+    if (a.deal)
+        deal_items(dealt, a.q_lens, a.kv_lens, a.B, a.H, a.Nq, a.Nk, a.tiles, a.causal, a.total_items, warp, kThreads / 32);
+    auto item_at = [&](int round) { return a.deal ? dealt[round] : item_of_round(a.total_items, round); };
+    __syncwarp();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -148,7 +155,7 @@ diff_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             Armed armed;
             bool ok = true;
             for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
-                const int item = item_of_round(a.total_items, round);
+                const int item = item_at(round);
                 if (item < 0) continue;
                 const DqItem c = decode_dq(a, item);
                 if (c.nhalf == 0) continue;
@@ -204,7 +211,7 @@ diff_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 return true;
             };
             for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
-                const int item = item_of_round(a.total_items, round);
+                const int item = item_at(round);
                 if (item < 0) continue;
                 const DqItem c = decode_dq(a, item);
                 if (c.nhalf == 0) continue;
@@ -252,7 +259,7 @@ diff_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         bool ok = true;
         uint32_t ic = 0, sc = 0;
         for (int round = 0; ok && round * (int)gridDim.x < a.total_items; ++round) {
-            const int item = item_of_round(a.total_items, round);
+            const int item = item_at(round);
             if (item < 0) continue;
             const DqItem c = decode_dq(a, item);
             const int t = c.t0 + r;
@@ -813,6 +820,7 @@ int launch_d(const DiffProblem &p, const DiffGrads &g) {
     if (dq_items > 0x3FFFFFFFll || dkv_items > 0x3FFFFFFFll) return TA_ERR_TOO_LARGE;
     a.total_items = (int)dq_items;
     a.tile_major = 2ull * p.B * p.H_kv * p.Nk * D * 2 <= (96ull << 20) ? 1 : 0;
+    a.deal = (p.q_lens || p.kv_lens) && p.B <= 32 && a.tile_major && a.total_items <= kDealt * num_sms ? 1 : 0;
     rc = launch_kernel(diff_tc_dq_kernel<D>, (unsigned)(a.total_items < num_sms ? a.total_items : num_sms), kThreads,
                        DqCfg<D>::kSmem, p.stream, true, mq, mg, mkh, mvh, a);
     if (rc != TA_OK) return rc;

@@ -361,6 +361,16 @@ def test_chunk_behind_a_long_cache(D, causal):
     check(1, 8, 2, 257, 2100, D, causal=causal, grad=False)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+def test_tiles_of_many_lengths(causal):
+    """More tiles than CTAs, several rounds of them, dealt by their lengths: entries of every length, some empty."""
+    gen = np.random.default_rng(6)
+    for B, H, N, D in ((32, 4, 300, 64), (33, 4, 140, 64), (7, 12, 400, 128)):
+        kl = [0, N, 1, 129, 128] + [int(x) for x in gen.integers(0, N + 1, B - 5)]
+        check(B, H, H // 2, N, N, D, causal=causal, ql=kl, kl=kl)
+    check(5, 12, 4, 520, 300, 64, causal=causal, ql=[520, 0, 130, 400, 257], kl=[10, 300, 300, 0, 200])
+
+
 @pytest.mark.parametrize("D", [64, 128])
 def test_many_requests_of_all_lengths(D):
     """More entries than a warp's lanes, with empty ones first, last and in a row."""
